@@ -1,0 +1,215 @@
+// mx4_quant.hip - rows to MX4 operands and back, for gfx950.
+//
+// All of it is bound by memory: quantizing reads 2 or 4 bytes per element and
+// writes 17/32; the arithmetic (a maximum over integer bits, and one scaled
+// conversion instruction per two elements, which rounds to nearest even and
+// saturates) hides behind the loads.
+//
+// A wave takes 16 rows and one step (256 elements) of K: lane s + 16 q holds
+// blocks q and q + 4 of row s, whole blocks, so that a block's scale needs no
+// other lane, its 16 code bytes are one store, and the wave's stores are whole
+// 1 KB runs of the operand.  The lane's reads are 64 (or 128) contiguous bytes
+// in 16-byte pieces; the lines that a piece leaves unread are read by the
+// same wave's next pieces from the L1 cache.
+#include "mx4.h"
+
+namespace apt {
+namespace {
+
+using namespace mx4;
+
+constexpr int kWave = 64;
+constexpr int kWaves = 4;
+
+template <class T>
+__global__ __launch_bounds__(kWave* kWaves) void quantize_kernel(const uint8_t* __restrict__ x, int rows, int K,
+                                                                 int64_t stride, Operand o) {
+  constexpr int kPieces = kBlock / T::kVec;
+  const int lane = threadIdx.x % kWave;
+  const int64_t unit = (int64_t)blockIdx.x * kWaves + threadIdx.x / kWave;
+  if (unit >= o.groups * o.steps) return;
+  const int s = lane % kGroup, q = lane / kGroup;
+  const int64_t g = unit / o.steps;
+  const int k0 = (int)(unit % o.steps) * kStep;
+  const int64_t row = g * kGroup + s;
+  const bool real = row < rows;
+  const uint8_t* const src = x + (real ? row : 0) * stride * T::kBytes;
+  u32x4 v[2][kPieces];
+  // (rows past the edge read the first row and store nothing)
+  if (k0 + kStep <= K) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int i = 0; i < kPieces; ++i) v[u][i] = load_whole<T>(src, k0 + (q + 4 * u) * kBlock + i * T::kVec);
+  } else {
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int i = 0; i < kPieces; ++i) v[u][i] = load_vector<T>(src, k0 + (q + 4 * u) * kBlock + i * T::kVec, K);
+  }
+  uint32_t bytes = 0u;
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    uint32_t m = 0u;
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) m = fold_magnitude<T>(m, v[u][i]);
+    const uint32_t byte = scale_byte<T>(widest<T>(m));
+    const float scale = scale_of(byte);
+    u32x4 c;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) c[i] = byte == 255u ? 0u : codes_of<T>(v[u] + i * kPieces / 4, scale);
+    if (real) *reinterpret_cast<u32x4*>(o.codes + (unit * 8 + q + 4 * u) * 256 + s * 16) = c;
+    bytes |= byte << (16 * u);
+  }
+  // blocks q, q + 4 are bytes 0, 2 (q < 2) or 1, 3 of the dword of half q mod 2
+  bytes |= (uint32_t)__shfl_xor((int)bytes, 32) << 8;
+  if (real && q < 2) *reinterpret_cast<uint32_t*>(o.scales + unit * kScaleBytes + q * 64 + s * 4) = bytes;
+}
+
+// Values of an operand.  A wave takes 16 rows and one step again; its lane l
+// takes eight elements of a row at a time, rows l / 32 + 2 i, so that its
+// stores are whole 512-byte (16-bit types) or 1 KB runs of two rows.
+template <class T>
+__global__ __launch_bounds__(kWave* kWaves) void dequantize_kernel(Operand o, int rows, int K, uint8_t* __restrict__ out) {
+  const int lane = threadIdx.x % kWave;
+  const int64_t unit = (int64_t)blockIdx.x * kWaves + threadIdx.x / kWave;
+  if (unit >= o.groups * o.steps) return;
+  const int64_t g = unit / o.steps;
+  const int p = lane % 32, b = p / 4;  // eighth of the step, its block
+  const int k = (int)(unit % o.steps) * kStep + p * 8;
+  uint32_t c[8], e[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int s = lane / 32 + 2 * i;
+    c[i] = *reinterpret_cast<const uint32_t*>(o.codes + (unit * 8 + b) * 256 + s * 16 + p % 4 * 4);
+    e[i] = o.scales[unit * kScaleBytes + b % 2 * 64 + s * 4 + b / 2];
+  }
+  if (k >= K) return;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int64_t row = g * kGroup + lane / 32 + 2 * i;
+    if (row >= rows) return;
+    float f[8];
+    const float scale = scale_of(e[i]);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const uint32_t n = c[i] >> (4 * j) & 15u;
+      // the fp32 of magnitude n = (exponent, mantissa): 1.m 2^(ee - 1), m / 2 for ee = 0
+      const uint32_t mag = n & 7u;
+      const float a = mag < 2u ? 0.5f * (float)mag : __builtin_bit_cast(float, (mag << 22) + (126u << 23));
+      f[j] = e[i] == 255u ? __builtin_nanf("") : (n & 8u ? -a : a) * scale;
+    }
+    const int64_t at = row * K + k;
+    if constexpr (T::kBytes == 4) {
+      float* const dst = reinterpret_cast<float*>(out) + at;
+      if (k + 8 <= K) {
+        u32x4 lo, hi;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          lo[j] = __builtin_bit_cast(uint32_t, f[j]);
+          hi[j] = __builtin_bit_cast(uint32_t, f[4 + j]);
+        }
+        reinterpret_cast<any_u32x4*>(dst)[0] = lo;
+        reinterpret_cast<any_u32x4*>(dst)[1] = hi;
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (k + j < K) dst[j] = f[j];
+      }
+    } else {
+      uint16_t* const dst = reinterpret_cast<uint16_t*>(out) + at;
+      uint16_t h[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) h[j] = T::from_float(f[j]);
+      if (k + 8 <= K) {
+        u32x4 v;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = (uint32_t)h[2 * j] | (uint32_t)h[2 * j + 1] << 16;
+        *reinterpret_cast<any_u32x4*>(dst) = v;
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (k + j < K) dst[j] = h[j];
+      }
+    }
+  }
+}
+
+// Row-major codes and scale bytes into the operand (or back), a thread per
+// block: once per model, so nothing of it is tuned.
+__global__ __launch_bounds__(256) void pack_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales,
+                                                   int rows, int K, Operand o) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t unit = i / 128;
+  if (unit >= o.groups * o.steps) return;
+  const int s = i % 16, b = (int)(i / 16 % 8);
+  const int64_t row = unit / o.steps * kGroup + s;
+  if (row >= rows) return;
+  const int k = (int)(unit % o.steps) * kStep + b * kBlock;
+  const int64_t row_bytes = ((int64_t)K + 1) / 2, blocks = ((int64_t)K + kBlock - 1) / kBlock;
+  u32x4 c = {0u, 0u, 0u, 0u};
+#pragma unroll
+  for (int j = 0; j < 16; ++j)
+    if (k + 2 * j < K) {
+      const uint32_t v = codes[row * row_bytes + k / 2 + j];
+      c[j / 4] |= (k + 2 * j + 1 < K ? v : v & 15u) << (8 * (j % 4));
+    }
+  *reinterpret_cast<u32x4*>(o.codes + (unit * 8 + b) * 256 + s * 16) = c;
+  o.scales[unit * kScaleBytes + b % 2 * 64 + s * 4 + b / 2] = k < K ? scales[row * blocks + k / kBlock] : 0;
+}
+
+__global__ __launch_bounds__(256) void unpack_kernel(Operand o, int rows, int K, uint8_t* __restrict__ codes,
+                                                     uint8_t* __restrict__ scales) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t unit = i / 128;
+  if (unit >= o.groups * o.steps) return;
+  const int s = i % 16, b = (int)(i / 16 % 8);
+  const int64_t row = unit / o.steps * kGroup + s;
+  const int k = (int)(unit % o.steps) * kStep + b * kBlock;
+  if (row >= rows || k >= K) return;
+  const int64_t row_bytes = ((int64_t)K + 1) / 2, blocks = ((int64_t)K + kBlock - 1) / kBlock;
+  const u32x4 c = *reinterpret_cast<const u32x4*>(o.codes + (unit * 8 + b) * 256 + s * 16);
+#pragma unroll
+  for (int j = 0; j < 16; ++j)
+    if (k + 2 * j < K) codes[row * row_bytes + k / 2 + j] = (uint8_t)(c[j / 4] >> (8 * (j % 4)));
+  scales[row * blocks + k / kBlock] = o.scales[unit * kScaleBytes + b % 2 * 64 + s * 4 + b / 2];
+}
+
+unsigned unit_blocks(const Operand& o) { return (unsigned)((o.groups * o.steps + kWaves - 1) / kWaves); }
+
+}  // namespace
+
+namespace mx4 {
+
+hipError_t launch_quantize(const void* x, int type, int rows, int K, int64_t stride, const Operand& o, hipStream_t s) {
+  const dim3 grid(unit_blocks(o)), block(kWave * kWaves);
+  const uint8_t* const src = static_cast<const uint8_t*>(x);
+  switch (type) {
+    case APT_TYPE_FP16: return launch_kernel(quantize_kernel<Half>, grid, block, 0, s, src, rows, K, stride, o);
+    case APT_TYPE_BF16: return launch_kernel(quantize_kernel<Bf16>, grid, block, 0, s, src, rows, K, stride, o);
+    default: return launch_kernel(quantize_kernel<Float>, grid, block, 0, s, src, rows, K, stride, o);
+  }
+}
+
+hipError_t launch_dequantize(const Operand& o, int rows, int K, int type, void* out, hipStream_t s) {
+  const dim3 grid(unit_blocks(o)), block(kWave * kWaves);
+  uint8_t* const dst = static_cast<uint8_t*>(out);
+  switch (type) {
+    case APT_TYPE_FP16: return launch_kernel(dequantize_kernel<Half>, grid, block, 0, s, o, rows, K, dst);
+    case APT_TYPE_BF16: return launch_kernel(dequantize_kernel<Bf16>, grid, block, 0, s, o, rows, K, dst);
+    default: return launch_kernel(dequantize_kernel<Float>, grid, block, 0, s, o, rows, K, dst);
+  }
+}
+
+hipError_t launch_pack(const uint8_t* codes, const uint8_t* scales, int rows, int K, const Operand& o, hipStream_t s) {
+  const dim3 grid((unsigned)((o.groups * o.steps + 1) / 2)), block(256);
+  return launch_kernel(pack_kernel, grid, block, 0, s, codes, scales, rows, K, o);
+}
+
+hipError_t launch_unpack(const Operand& o, int rows, int K, uint8_t* codes, uint8_t* scales, hipStream_t s) {
+  const dim3 grid((unsigned)((o.groups * o.steps + 1) / 2)), block(256);
+  return launch_kernel(unpack_kernel, grid, block, 0, s, o, rows, K, codes, scales);
+}
+
+}  // namespace mx4
+}  // namespace apt

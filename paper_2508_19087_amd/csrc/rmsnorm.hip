@@ -1,0 +1,387 @@
+// rmsnorm.hip - RMS norm of rows with the residual's addition in front and the
+// operand of a quantized product behind (q-bit codes with a scale per row, or
+// MX4), for gfx950.
+//
+// Bound by memory: 2 bytes per element of x and residual in, 2 of h and 1 (or
+// 17/32) of the operand out.  A row is one workgroup's and stays in registers
+// between its passes (sum of squares, largest magnitude of y, codes), each
+// thread holding NV vectors of 8 elements; rows longer than the registers
+// reach (NV = 0) are read again in each pass.
+//
+// The sum of squares runs in fp64.  A quantizer is a step function, and a y
+// that moved by one rounding with the order of its row's sum would now and then
+// move a code; squares of 11-bit values and their sums are exact to 2^-53 here,
+// so the order never shows in f, and y and its codes follow from f by single
+// IEEE operations.
+//
+// Codes: with h = y / (2 s), code = floor(h).  y and s have at most 11
+// significant bits, so an h that is no integer lies 2^-18 of itself or more
+// away from one, while fp32(y * fp32(0.5 / s)) is within 2^-23 of h: the bias
+// |h| 2^-20 lifts every integer over its own border and nothing else over the
+// next.
+#include "mx4.h"
+
+namespace apt {
+namespace {
+
+using namespace mx4;
+
+constexpr int kWave = 64;
+constexpr int kMaxWaves = 16;
+
+struct NormArgs {
+  int M, K;
+  const uint8_t* x;
+  int64_t x_stride;  // elements
+  const uint8_t* residual;
+  int64_t r_stride;
+  const uint8_t* gain;
+  double eps;
+  uint8_t* h;
+  uint8_t* y;
+  int q;
+  int8_t* codes;
+  uint16_t* scale;
+  Operand mx;
+};
+
+// Eight elements of fp32 from a vector of 16-bit ones, and back.
+template <class T>
+__device__ __forceinline__ void spread(u32x4 v, float (&f)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) f[i] = T::to_float((uint16_t)(v[i / 2] >> (16 * (i % 2))));
+}
+template <class T>
+__device__ __forceinline__ u32x4 join(const float (&f)[8]) {
+  u32x4 v;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = (uint32_t)T::from_float(f[2 * i]) | (uint32_t)T::from_float(f[2 * i + 1]) << 16;
+  return v;
+}
+
+__device__ __forceinline__ void store_vector(uint8_t* row, int k, int K, u32x4 v) {
+  if (k + 8 <= K) {
+    *reinterpret_cast<any_u32x4*>(row + (int64_t)k * 2) = v;
+  } else {
+    uint16_t* const p = reinterpret_cast<uint16_t*>(row);
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (k + i < K) p[k + i] = (uint16_t)(v[i / 2] >> (16 * (i % 2)));
+  }
+}
+
+// Sum and largest value over the workgroup; `lds` holds a value per wave.
+__device__ __forceinline__ double block_sum(double v, double* lds) {
+  for (int off = 1; off < kWave; off <<= 1) v += __shfl_xor(v, off);
+  if (threadIdx.x % kWave == 0) lds[threadIdx.x / kWave] = v;
+  __syncthreads();
+  double sum = 0.0;
+  for (int w = 0; w < (int)blockDim.x / kWave; ++w) sum += lds[w];
+  return sum;
+}
+__device__ __forceinline__ uint32_t block_max(uint32_t v, uint32_t* lds) {
+  for (int off = 1; off < kWave; off <<= 1) v = max(v, (uint32_t)__shfl_xor((int)v, off));
+  if (threadIdx.x % kWave == 0) lds[threadIdx.x / kWave] = v;
+  __syncthreads();
+  uint32_t m = 0u;
+  for (int w = 0; w < (int)blockDim.x / kWave; ++w) m = max(m, lds[w]);
+  return m;
+}
+
+// A row's codes from its largest magnitude.
+struct CodeScale {
+  float rh;        // 0.5 / s
+  uint16_t bits;   // s
+  bool bad;
+  template <class T>
+  __device__ __forceinline__ void set(uint32_t m, int q) {
+    const float top = (float)((1 << q) - 1);
+    const _Float16 s = (_Float16)__fdiv_rn(T::to_float((uint16_t)m), top);
+    bits = __builtin_bit_cast(uint16_t, s);
+    bad = m >= T::kInf || bits >= 0x7C00u;
+    if (bad) bits = 0x7E00u;
+    rh = !bad && (float)s > 0.0f ? __fdiv_rn(0.5f, (float)s) : 0.0f;
+  }
+  // code of y (0 in a bad row), as a byte
+  __device__ __forceinline__ uint32_t code(float y, int lo, int hi) const {
+    const float h = y * rh;
+    int c;
+    asm("v_cvt_flr_i32_f32 %0, %1" : "=v"(c) : "v"(__builtin_fmaf(__builtin_fabsf(h), 0x1p-20f, h)));
+    return (uint32_t)min(max(c, lo), hi) & 255u;
+  }
+};
+
+// T: element type; NV: vectors of 8 elements held per thread (0: none, the row
+// is read again in each pass); kCodes: q-bit codes, else MX4.
+template <class T, int NV, bool kCodes>
+__global__ __launch_bounds__(kWave* kMaxWaves) void rmsnorm_kernel(NormArgs a) {
+  __shared__ double lds_sum[kMaxWaves];
+  __shared__ uint32_t lds_max[kMaxWaves];
+  const int tid = threadIdx.x, K = a.K;
+  // MX4: the 16 rows of a group share the operand's lines, and workgroups are
+  // dealt round-robin to the 8 XCDs: group g's rows go to XCD g mod 8
+  const int64_t row = kCodes ? (int64_t)blockIdx.x
+                             : (int64_t)(blockIdx.x / 128) * 128 + blockIdx.x % 8 * 16 + blockIdx.x / 8 % 16;
+  if (row >= a.M) return;
+  const uint8_t* const x = a.x + row * a.x_stride * 2;
+  const uint8_t* const r = a.residual != nullptr ? a.residual + row * a.r_stride * 2 : nullptr;
+  uint8_t* const hrow = a.h != nullptr ? a.h + row * K * 2 : nullptr;
+  uint8_t* const yrow = a.y != nullptr ? a.y + row * K * 2 : nullptr;
+  // elements that are written: MX4 rows end on a step
+  const int end = kCodes ? K : (K + kStep - 1) / kStep * kStep;
+  const int vectors = (end + 7) / 8;
+
+  auto sum_of = [&](u32x4 xv, u32x4 rv) __attribute__((always_inline)) {
+    if (r == nullptr) return xv;
+    float f[8], e[8];
+    spread<T>(xv, f);
+    spread<T>(rv, e);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] += e[i];
+    return join<T>(f);
+  };
+  auto squares = [&](u32x4 h) __attribute__((always_inline)) {
+    float f[8];
+    spread<T>(h, f);
+    double s = 0.0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s = __builtin_fma((double)f[i], (double)f[i], s);
+    return s;
+  };
+  auto normed = [&](u32x4 h, u32x4 g, float f) __attribute__((always_inline)) {
+    float v[8], e[8];
+    spread<T>(h, v);
+    spread<T>(g, e);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      v[i] *= f;
+      if (a.gain != nullptr) v[i] *= e[i];
+    }
+    return join<T>(v);
+  };
+  auto factor = [&](double sum) __attribute__((always_inline)) { return (float)(1.0 / __builtin_sqrt(sum / (double)K + a.eps)); };
+  const int lo = -(1 << (a.q - 1)), hi = (1 << (a.q - 1)) - 1;
+  auto store_codes = [&](int k, u32x4 y, const CodeScale& cs) __attribute__((always_inline)) {
+    float f[8];
+    spread<T>(y, f);
+    u32x2 c = {0u, 0u};
+    if (!cs.bad) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) c[i / 4] |= cs.code(f[i], lo, hi) << (8 * (i % 4));
+    }
+    uint8_t* const dst = reinterpret_cast<uint8_t*>(a.codes) + row * K + k;
+    if (k + 8 <= K) {
+      typedef uint32_t any_u32x2 __attribute__((ext_vector_type(2), aligned(1)));
+      *reinterpret_cast<any_u32x2*>(dst) = c;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (k + i < K) dst[i] = (uint8_t)(c[i / 4] >> (8 * (i % 4)));
+    }
+  };
+  // (the four lanes of a block are neighbours, active together)
+  auto store_mx4 = [&](int k, u32x4 y) __attribute__((always_inline)) {
+    uint32_t m = fold_magnitude<T>(0u, y);
+    m = widest<T>(m);
+    m = max(m, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0xB1, 0xF, 0xF, false));
+    m = max(m, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0x4E, 0xF, 0xF, false));
+    const uint32_t byte = scale_byte<T>(m);
+    const uint32_t c = byte == 255u ? 0u : codes_of<T>(&y, scale_of(byte));
+    const int64_t unit = row / kGroup * a.mx.steps + k / kStep;
+    const int s = (int)(row % kGroup), b = k % kStep / kBlock;
+    *reinterpret_cast<uint32_t*>(a.mx.codes + (unit * 8 + b) * 256 + s * 16 + k % kBlock / 2) = c;
+    if (k % kBlock == 0) a.mx.scales[unit * kScaleBytes + b % 2 * 64 + s * 4 + b / 2] = (uint8_t)byte;
+  };
+
+  const u32x4 none = {0u, 0u, 0u, 0u};
+  if constexpr (NV > 0) {
+    u32x4 v[NV], g[NV];
+    {
+      u32x4 rv[NV];
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        const int k = (i * (int)blockDim.x + tid) * 8;
+        v[i] = load_vector<T>(x, k, K);
+        rv[i] = r != nullptr ? load_vector<T>(r, k, K) : none;
+        g[i] = a.gain != nullptr ? load_vector<T>(a.gain, k, K) : none;
+      }
+#pragma unroll
+      for (int i = 0; i < NV; ++i) v[i] = sum_of(v[i], rv[i]);
+    }
+    double sum = 0.0;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int k = (i * (int)blockDim.x + tid) * 8;
+      if (hrow != nullptr) store_vector(hrow, k, K, v[i]);
+      sum += squares(v[i]);
+    }
+    const float f = factor(block_sum(sum, lds_sum));
+    uint32_t m = 0u;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int k = (i * (int)blockDim.x + tid) * 8;
+      v[i] = normed(v[i], g[i], f);
+      if (k + 8 > K) {  // (0 * an infinite or NaN f: the elements behind K stay 0)
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (k + j >= K) v[i][j / 2] &= j % 2 ? 0x0000FFFFu : 0xFFFF0000u;
+      }
+      if (yrow != nullptr) store_vector(yrow, k, K, v[i]);
+      if (kCodes) m = fold_magnitude<T>(m, v[i]);
+      else if (k < end) store_mx4(k, v[i]);
+    }
+    if constexpr (kCodes) {
+      CodeScale cs;
+      cs.set<T>(block_max(widest<T>(m), lds_max), a.q);
+#pragma unroll
+      for (int i = 0; i < NV; ++i) store_codes((i * (int)blockDim.x + tid) * 8, v[i], cs);
+      if (tid == 0) a.scale[row] = cs.bits;
+    }
+  } else {
+    auto load_h = [&](int k) __attribute__((always_inline)) {
+      return sum_of(load_vector<T>(x, k, K), r != nullptr ? load_vector<T>(r, k, K) : none);
+    };
+    double sum = 0.0;
+    for (int i = tid; i < vectors; i += (int)blockDim.x) {
+      const u32x4 h = load_h(i * 8);
+      if (hrow != nullptr) store_vector(hrow, i * 8, K, h);
+      sum += squares(h);
+    }
+    const float f = factor(block_sum(sum, lds_sum));
+    // (h may have replaced x or the residual: it is read back, by the thread that wrote it)
+    auto load_y = [&](int k) __attribute__((always_inline)) {
+      const u32x4 h = hrow != nullptr ? load_vector<T>(hrow, k, K) : load_h(k);
+      u32x4 y = normed(h, a.gain != nullptr ? load_vector<T>(a.gain, k, K) : none, f);
+      if (k + 8 > K) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (k + j >= K) y[j / 2] &= j % 2 ? 0x0000FFFFu : 0xFFFF0000u;
+      }
+      return y;
+    };
+    uint32_t m = 0u;
+    for (int i = tid; i < vectors; i += (int)blockDim.x) {
+      const u32x4 y = load_y(i * 8);
+      if (yrow != nullptr) store_vector(yrow, i * 8, K, y);
+      if (kCodes) m = fold_magnitude<T>(m, y);
+      else store_mx4(i * 8, y);
+    }
+    if constexpr (kCodes) {
+      CodeScale cs;
+      cs.set<T>(block_max(widest<T>(m), lds_max), a.q);
+      for (int i = tid; i < vectors; i += (int)blockDim.x) store_codes(i * 8, load_y(i * 8), cs);
+      if (tid == 0) a.scale[row] = cs.bits;
+    }
+  }
+}
+
+// (2 code + 1) scale, eight elements of a row per thread: bound by memory, 1
+// byte in and 2 or 4 out per element.
+template <class T>
+__global__ __launch_bounds__(256) void dequantize_codes_kernel(const int8_t* __restrict__ codes,
+                                                               const uint16_t* __restrict__ scale, int K, int parts,
+                                                               uint8_t* __restrict__ out) {
+  const int64_t row = blockIdx.x / (unsigned)parts;
+  const int k = ((int)(blockIdx.x % (unsigned)parts) * 256 + (int)threadIdx.x) * 8;
+  if (k >= K) return;
+  const float s = Half::to_float(scale[row]);
+  const int8_t* const src = codes + row * K + k;
+  const bool whole = k + 8 <= K;
+  typedef uint32_t any_u32x2 __attribute__((ext_vector_type(2), aligned(1)));
+  u32x2 c = {0u, 0u};
+  if (whole) {
+    c = *reinterpret_cast<const any_u32x2*>(src);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (k + i < K) c[i / 4] |= (uint32_t)(uint8_t)src[i] << (8 * (i % 4));
+  }
+  float f[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) f[i] = (float)(2 * (int)(int8_t)(c[i / 4] >> (8 * (i % 4))) + 1) * s;
+  if constexpr (T::kBytes == 4) {
+    float* const dst = reinterpret_cast<float*>(out) + row * K + k;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (whole || k + i < K) dst[i] = f[i];
+  } else {
+    store_vector(out + row * K * 2, k, K, join<T>(f));
+  }
+}
+
+template <class T, bool kCodes>
+hipError_t launch_norm_of(const NormArgs& a, int64_t rows, hipStream_t s) {
+  // rows of the launch, by whole groups of 128 for the MX4 mapping
+  const unsigned grid = (unsigned)(kCodes ? rows : (rows + 127) / 128 * 128);
+  const int vectors = (kCodes ? a.K + 7 : (a.K + kStep - 1) / kStep * kStep) / 8;
+  auto threads = [&](int per) { return dim3((unsigned)((vectors + per * kWave - 1) / (per * kWave) * kWave)); };
+  if (vectors <= 512) return launch_kernel(rmsnorm_kernel<T, 1, kCodes>, dim3(grid), threads(1), 0, s, a);
+  if (vectors <= 2048) return launch_kernel(rmsnorm_kernel<T, 2, kCodes>, dim3(grid), threads(2), 0, s, a);
+  if (vectors <= 4096) return launch_kernel(rmsnorm_kernel<T, 4, kCodes>, dim3(grid), threads(4), 0, s, a);
+  return launch_kernel(rmsnorm_kernel<T, 0, kCodes>, dim3(grid), dim3(kWave * kMaxWaves), 0, s, a);
+}
+
+// A launch holds fewer than 2^32 threads: at 1024 a row, this many rows (whole
+// groups of 128).
+constexpr int64_t kLaunchRows = (int64_t)1 << 21;
+
+}  // namespace
+
+namespace mx4 {
+
+hipError_t launch_rmsnorm(int M, int K, int type, const void* x, int64_t x_stride, const void* residual, int64_t r_stride,
+                          const void* gain, double eps, void* h, void* y, int q, int8_t* codes, uint16_t* scale,
+                          const Operand* mx, hipStream_t s) {
+  for (int64_t r0 = 0; r0 < M; r0 += kLaunchRows) {
+    const int64_t rows = M - r0 < kLaunchRows ? M - r0 : kLaunchRows;
+    NormArgs a{};
+    a.M = (int)rows;
+    a.K = K;
+    a.x = static_cast<const uint8_t*>(x) + r0 * x_stride * 2;
+    a.x_stride = x_stride;
+    if (residual != nullptr) a.residual = static_cast<const uint8_t*>(residual) + r0 * r_stride * 2;
+    a.r_stride = r_stride;
+    a.gain = static_cast<const uint8_t*>(gain);
+    a.eps = eps;
+    if (h != nullptr) a.h = static_cast<uint8_t*>(h) + r0 * K * 2;
+    if (y != nullptr) a.y = static_cast<uint8_t*>(y) + r0 * K * 2;
+    a.q = mx == nullptr ? q : 1;
+    hipError_t e;
+    if (mx == nullptr) {
+      a.codes = codes + r0 * K;
+      a.scale = scale + r0;
+      e = type == APT_TYPE_FP16 ? launch_norm_of<Half, true>(a, rows, s) : launch_norm_of<Bf16, true>(a, rows, s);
+    } else {
+      a.mx = *mx;
+      a.mx.codes += r0 / kGroup * mx->steps * kCodeBytes;
+      a.mx.scales += r0 / kGroup * mx->steps * kScaleBytes;
+      e = type == APT_TYPE_FP16 ? launch_norm_of<Half, false>(a, rows, s) : launch_norm_of<Bf16, false>(a, rows, s);
+    }
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+hipError_t launch_dequantize_codes(const int8_t* codes, const uint16_t* scale, int M, int K, int type, void* out,
+                                   hipStream_t s) {
+  const int parts = (K + 2047) / 2048;
+  const int64_t most = ((int64_t)1 << 23) / parts > 0 ? ((int64_t)1 << 23) / parts : 1;  // rows of a launch
+  const int size = type == APT_TYPE_FP32 ? 4 : 2;
+  for (int64_t r0 = 0; r0 < M; r0 += most) {
+    const int64_t rows = M - r0 < most ? M - r0 : most;
+    const dim3 grid((unsigned)(rows * parts)), block(256);
+    const int8_t* const c = codes + r0 * K;
+    uint8_t* const o = static_cast<uint8_t*>(out) + r0 * K * size;
+    hipError_t e;
+    switch (type) {
+      case APT_TYPE_FP16: e = launch_kernel(dequantize_codes_kernel<Half>, grid, block, 0, s, c, scale + r0, K, parts, o); break;
+      case APT_TYPE_BF16: e = launch_kernel(dequantize_codes_kernel<Bf16>, grid, block, 0, s, c, scale + r0, K, parts, o); break;
+      default: e = launch_kernel(dequantize_codes_kernel<Float>, grid, block, 0, s, c, scale + r0, K, parts, o); break;
+    }
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+}  // namespace mx4
+}  // namespace apt

@@ -1,0 +1,261 @@
+"""MX4 operands and their product on the GPU against the 64-bit oracle."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2508_19087_amd as apt
+from oracle import mx_oracle as ref
+
+pytestmark = pytest.mark.gpu
+
+TYPES = {"fp16": torch.float16, "bf16": torch.bfloat16, "fp32": torch.float32}
+
+
+def rows(seed, M, K, kind="fp16", spread=3.0):
+    """Values of `kind` as float64, magnitudes over several powers of two, some zeros."""
+    g = np.random.default_rng(seed)
+    x = g.standard_normal((M, K)) * np.exp(g.uniform(-spread, spread, (M, K)))
+    x[g.random((M, K)) < 0.05] = 0.0
+    return ref.rounded(x, kind)
+
+
+def dev(x, kind):
+    return torch.from_numpy(np.ascontiguousarray(x)).to(TYPES[kind]).cuda()
+
+
+def f64(t):
+    torch.cuda.synchronize()
+    return t.double().cpu().numpy()
+
+
+def random_mx4(seed, R, K, low=120, high=134):
+    """(codes, scales) at random."""
+    g = np.random.default_rng(seed)
+    return (g.integers(0, 16, (R, K)).astype(np.uint8), g.integers(low, high, (R, ref.blocks(K))).astype(np.uint8))
+
+
+def packed(codes, scales):
+    return apt.mx4_pack(torch.from_numpy(ref.nibbles(codes)).cuda(), torch.from_numpy(scales).cuda(), codes.shape[1])
+
+
+def same_operand(op, codes, scales):
+    want, written = ref.operand(codes, scales)
+    got = op.data.cpu().numpy()
+    assert np.array_equal(got[written], want[written])
+
+
+SHAPES = [(1, 1), (1, 31), (2, 32), (3, 33), (15, 255), (16, 256), (17, 257), (33, 1000), (5, 4096), (70, 2999)]
+
+
+@pytest.mark.parametrize("R,K", SHAPES)
+def test_pack_and_unpack(R, K):
+    codes, scales = random_mx4(R * 7 + K, R, K, 0, 256)
+    op = packed(codes, scales)
+    torch.cuda.synchronize()
+    same_operand(op, codes, scales)
+    c, s = apt.mx4_unpack(op)
+    torch.cuda.synchronize()
+    assert np.array_equal(c.cpu().numpy(), ref.nibbles(codes)) and np.array_equal(s.cpu().numpy(), scales)
+
+
+def test_pack_ignores_a_nibble_behind_the_row():
+    codes, scales = random_mx4(1, 3, 33)
+    n = ref.nibbles(codes)
+    n[:, -1] |= 0xF0
+    op = apt.mx4_pack(torch.from_numpy(n).cuda(), torch.from_numpy(scales).cuda(), 33)
+    torch.cuda.synchronize()
+    same_operand(op, codes, scales)
+
+
+@pytest.mark.parametrize("kind", ["fp16", "bf16", "fp32"])
+@pytest.mark.parametrize("R,K", SHAPES)
+def test_quantize_bits(R, K, kind):
+    x = rows(R + K, R, K, kind)
+    op = apt.mx4_quantize(dev(x, kind))
+    torch.cuda.synchronize()
+    same_operand(op, *ref.quantize(x))
+
+
+@pytest.mark.parametrize("kind", ["fp16", "bf16", "fp32"])
+def test_quantize_borders_and_extremes(kind):
+    """Every tie and its neighbours at many scales, zeros, the type's ends, infinities and NaN."""
+    info = torch.finfo(TYPES[kind])
+    ties = np.array([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 6.0, 7.0])
+    eps = {"fp16": 2.0 ** -10, "bf16": 2.0 ** -7, "fp32": 2.0 ** -23}[kind]
+    row = np.concatenate([ties, -ties, ties * (1 + eps), ties * (1 - eps / 2)])[:31]
+    x = np.zeros((48, 64))
+    for i in range(20):
+        e = {"fp16": -12, "bf16": -60, "fp32": -60}[kind] + i * {"fp16": 1, "bf16": 6, "fp32": 6}[kind]
+        x[i, 0], x[i, 1:32] = 2.0 ** (e + 2), row * 2.0 ** e
+        x[i, 32] = -7.99 * 2.0 ** e
+    x[20, 3] = float(info.max)
+    x[21, 5] = -float(info.max)
+    x[22, 7] = float(info.tiny)
+    x[23, 9] = float(info.smallest_normal) / 4
+    x[24, 33] = np.inf
+    x[25, 2] = -np.inf
+    x[26, 34], x[26, 35] = np.nan, 3.0
+    x[27] = -0.0
+    x[28] = {"fp16": 2.0 ** -24, "bf16": 2.0 ** -133, "fp32": 2.0 ** -149}[kind]
+    x[29, :32] = np.arange(32) * {"fp16": 2.0 ** -24, "bf16": 2.0 ** -133, "fp32": 2.0 ** -149}[kind]
+    x[30, :32] = np.arange(32) * {"fp16": 2.0 ** -24, "bf16": 2.0 ** -130, "fp32": 2.0 ** -130}[kind]
+    x = ref.rounded(x, kind)
+    t = dev(x, kind)
+    assert np.array_equal(np.nan_to_num(f64(t), nan=1.5), np.nan_to_num(x, nan=1.5))  # subnormals survive the way
+    op = apt.mx4_quantize(t)
+    torch.cuda.synchronize()
+    same_operand(op, *ref.quantize(x))
+
+
+def test_quantize_strided_unaligned_and_broadcast_rows():
+    x = rows(5, 20, 300)
+    wide = torch.zeros(20, 1001, dtype=torch.float16, device="cuda")
+    want = ref.quantize(x)
+    for at in (0, 1, 3, 8, 700):
+        wide[:, at:at + 300] = dev(x, "fp16")
+        op = apt.mx4_quantize(wide[:, at:at + 300])
+        torch.cuda.synchronize()
+        same_operand(op, *want)
+    op = apt.mx4_quantize(dev(x.T, "fp16").t())  # columns apart: copied
+    torch.cuda.synchronize()
+    same_operand(op, *want)
+    op = apt.mx4_quantize(dev(x[:1], "fp16").expand(20, 300))
+    torch.cuda.synchronize()
+    same_operand(op, *ref.quantize(np.repeat(x[:1], 20, axis=0)))
+
+
+def test_quantize_leaves_the_padding_rows():
+    x = rows(6, 5, 300)
+    n = apt.apt_mx4_bytes(5, 300)
+    buf = torch.full((n, ), 0xA5, dtype=torch.uint8, device="cuda")
+    t = dev(x, "fp16")
+    apt.check(apt.apt_mx4_quantize(t.data_ptr(), apt.APT_TYPE_FP16, 5, 300, 300, buf.data_ptr(),
+                                   torch.cuda.current_stream().cuda_stream), "apt_mx4_quantize")
+    torch.cuda.synchronize()
+    want, written = ref.operand(*ref.quantize(x))
+    got = buf.cpu().numpy()
+    assert np.array_equal(got[written], want[written]) and (got[~written] == 0xA5).all()
+
+
+@pytest.mark.parametrize("kind", ["fp16", "bf16", "fp32"])
+@pytest.mark.parametrize("R,K", SHAPES)
+def test_dequantize(R, K, kind):
+    codes, scales = random_mx4(R + 3 * K, R, K, 100, 150)
+    scales[0, 0] = 255
+    got = f64(apt.mx4_dequantize(packed(codes, scales), TYPES[kind]))
+    assert np.array_equal(got, ref.rounded(ref.values(codes, scales), kind), equal_nan=True)
+
+
+def test_dequantize_every_scale():
+    codes = np.tile(np.arange(16, dtype=np.uint8), (256, 2))
+    scales = np.arange(256, dtype=np.uint8)[:, None]
+    op = packed(codes, scales)
+    v = ref.values(codes, scales)
+    for kind in ("fp16", "bf16", "fp32"):
+        assert np.array_equal(f64(apt.mx4_dequantize(op, TYPES[kind])), ref.rounded(v, kind), equal_nan=True)
+
+
+# ---- the product --------------------------------------------------------------------
+
+def check_product(got, a, w, K, kind, what=""):
+    C, T = ref.product(a, w)
+    low, high = ref.product_bounds(C, T, K, kind)
+    got = f64(got)
+    bad = ~((got >= low) & (got <= high))
+    assert not bad.any(), "%s: %d outputs, the first %g for %g" % (what, bad.sum(), got[bad][0], C[bad][0])
+
+
+GEMM = [(1, 1, 1), (1, 16, 32), (1, 1000, 4096), (2, 33, 31), (3, 129, 257), (8, 512, 1000), (15, 64, 256),
+        (16, 512, 512), (17, 100, 513), (31, 257, 96), (32, 128, 2048), (33, 200, 300), (64, 1000, 2999),
+        (65, 96, 128), (100, 384, 777), (128, 256, 1024), (130, 513, 640), (200, 700, 96), (256, 256, 5000),
+        (300, 400, 1500), (513, 130, 257)]
+
+
+@pytest.mark.parametrize("kind", ["fp16", "bf16", "fp32"])
+@pytest.mark.parametrize("M,N,K", GEMM)
+def test_gemm(M, N, K, kind):
+    a, w = random_mx4(M + K, M, K), random_mx4(N + 2 * K, N, K)
+    got = apt.mx4_gemm(packed(*a), packed(*w), TYPES[kind])
+    assert got.shape == (M, N) and got.dtype == TYPES[kind]
+    check_product(got, ref.values(*a), ref.values(*w), K, kind, str((M, N, K)))
+
+
+@pytest.mark.parametrize("M,N,K", GEMM + [(1, 11008, 4096), (8, 4096, 11008), (1024, 1024, 1024), (2100, 300, 512)])
+def test_gemm_is_exact_where_sums_fit(M, N, K):
+    """Scales of 1 or 2: every partial sum is a multiple of 1/4 below 2^22 (36 * 4 * 11008 < 2^21), so fp32 holds it."""
+    a, w = random_mx4(M, M, K, 127, 129), random_mx4(N, N, K, 127, 129)
+    got = f64(apt.mx4_gemm(packed(*a), packed(*w), torch.float32))
+    va, vw = torch.from_numpy(ref.values(*a)).cuda(), torch.from_numpy(ref.values(*w)).cuda()
+    assert np.array_equal(got, f64(va @ vw.t()))
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 300, 4096), (40, 64, 4096), (200, 130, 1000)])
+def test_gemm_wide_scales(M, N, K):
+    """Block scales over the whole range of the type's exponents that fp32 outputs hold."""
+    a, w = random_mx4(M, M, K, 90, 170), random_mx4(N, N, K, 90, 160)
+    check_product(apt.mx4_gemm(packed(*a), packed(*w), torch.float32), ref.values(*a), ref.values(*w), K, "fp32")
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 70, 300), (20, 70, 300), (150, 300, 600)])
+def test_gemm_nan_scales_stay_in_their_rows(M, N, K):
+    a, w = random_mx4(1, M, K), random_mx4(2, N, K)
+    a[1][M // 2, 0] = 255
+    w[1][N - 1, -1] = 255
+    got = f64(apt.mx4_gemm(packed(*a), packed(*w), torch.float32))
+    nan = np.isnan(got)
+    want = np.zeros((M, N), dtype=bool)
+    want[M // 2], want[:, N - 1] = True, True
+    assert np.array_equal(nan, want)
+    low, high = ref.product_bounds(*ref.product(ref.values(*a), ref.values(*w)), K, "fp32")
+    assert ((got >= low) & (got <= high))[~want].all()
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 70, 300), (20, 70, 300), (150, 300, 600)])
+def test_gemm_reads_no_padding(M, N, K):
+    """Whatever the padding rows of the buffers hold, also NaN scales, does not show."""
+    a, w = random_mx4(1, M, K), random_mx4(2, N, K)
+    pa, pw = packed(*a), packed(*w)
+    want = apt.mx4_gemm(pa, pw, torch.float32)
+    for p, (c, s) in ((pa, a), (pw, w)):
+        buf, written = ref.operand(c, s)
+        buf[~written] = 0xFF
+        p.data.copy_(torch.from_numpy(buf))
+    got = apt.mx4_gemm(pa, pw, torch.float32)
+    assert torch.equal(got, want)
+
+
+def test_gemm_saturates_outputs_as_rounding_does():
+    codes = np.full((1, 256), 7, dtype=np.uint8)
+    big = packed(codes, np.full((1, 8), 140, dtype=np.uint8))
+    assert f64(apt.mx4_gemm(big, big, torch.float16))[0, 0] == np.inf
+    assert f64(apt.mx4_gemm(big, big, torch.float32))[0, 0] == 256 * 36 * 2.0 ** 26
+    huge = packed(codes, np.full((1, 8), 254, dtype=np.uint8))
+    assert f64(apt.mx4_gemm(huge, huge, torch.bfloat16))[0, 0] == np.inf
+
+
+@pytest.mark.parametrize("x_kind,kind", [("fp16", "fp16"), ("bf16", "bf16"), ("fp32", "fp32"), ("bf16", "fp32")])
+@pytest.mark.parametrize("M,N,K", [(1, 1, 1), (1, 1000, 4096), (1, 4096, 11008), (2, 200, 300), (4, 700, 1000),
+                                   (5, 64, 257), (8, 130, 2048), (16, 512, 512), (40, 300, 999), (200, 513, 1000)])
+def test_gemm_act_equals_quantize_then_gemm(M, N, K, x_kind, kind):
+    x = rows(M + N + K, M, K, x_kind, spread=1.0)
+    w = random_mx4(N, N, K, 118, 124)
+    pw, t = packed(*w), dev(x, x_kind)
+    got = apt.mx4_gemm_act(t, pw, TYPES[kind])
+    assert torch.equal(got, apt.mx4_gemm(apt.mx4_quantize(t), pw, TYPES[kind]))
+    check_product(got, ref.values(*ref.quantize(x)), ref.values(*w), K, kind)
+
+
+@pytest.mark.parametrize("M", [1, 3, 40])
+def test_gemm_act_strides_and_bad_rows(M):
+    """Rows inside a wider tensor at an odd element; a NaN reaches its row alone."""
+    K, N = 300, 100
+    x = rows(M, M, K)
+    wide = torch.full((M, 777), float("nan"), dtype=torch.float16, device="cuda")
+    wide[:, 5:5 + K] = dev(x, "fp16")
+    w = random_mx4(3, N, K)
+    pw = packed(*w)
+    want = apt.mx4_gemm_act(dev(x, "fp16"), pw, torch.float32)
+    assert torch.equal(apt.mx4_gemm_act(wide[:, 5:5 + K], pw, torch.float32), want)
+    wide[M - 1, 5 + K - 1] = float("inf")
+    got = apt.mx4_gemm_act(wide[:, 5:5 + K], pw, torch.float32)
+    assert torch.isnan(got[M - 1]).all() and torch.equal(got[:M - 1], want[:M - 1])

@@ -1,0 +1,129 @@
+"""Host-side checks of include/apt_mx.h (no kernel launches): symbols, sizes, and refusals, which come
+before anything reaches the GPU."""
+import math
+
+import pytest
+import torch
+
+import paper_2508_19087_amd as apt
+from paper_2508_19087_amd import mx
+
+BAD, UNSUPPORTED, NO_SPACE = apt.APT_ERR_INVALID_ARG, apt.APT_ERR_UNSUPPORTED, apt.APT_ERR_WORKSPACE
+F16, BF16, F32 = apt.APT_TYPE_FP16, apt.APT_TYPE_BF16, apt.APT_TYPE_FP32
+P = 1 << 20  # an address that no refused call looks at
+
+
+def test_exports_every_declared_symbol():
+    names = apt.mx_header_functions()
+    assert set(names) == set(mx._SIGNATURES)
+    for n in names:
+        assert hasattr(apt.lib(), n), n
+        assert callable(getattr(apt, n)), n
+
+
+@pytest.mark.parametrize("rows,K,want", [
+    (1, 1, 2176), (16, 256, 2176), (17, 256, 2 * 2176), (16, 257, 2 * 2176), (11008, 4096, 688 * 16 * 2176),
+    (0, 5, 0), (5, 0, 0), (-1, 5, 0), (5, -1, 0), (2 ** 31 - 1, 1, 2 ** 27 * 2176)])
+def test_bytes(rows, K, want):
+    assert apt.apt_mx4_bytes(rows, K) == want
+
+
+@pytest.mark.parametrize("bad", [
+    dict(rows=0), dict(K=0), dict(rows=-3), dict(x=None), dict(mx=None), dict(mx=P + 8), dict(x=P + 1),
+    dict(type=0), dict(type=4), dict(stride=99), dict(type=F32, x=P + 2)])
+def test_quantize_refuses(bad):
+    a = dict(x=P, type=F16, rows=3, K=100, stride=100, mx=P, stream=None) | bad
+    assert apt.apt_mx4_quantize(**a) == BAD
+
+
+def test_quantize_limits():
+    assert apt.apt_mx4_quantize(P, F16, 1, 2 ** 30 + 1, 2 ** 31, P, None) == UNSUPPORTED
+    assert apt.apt_mx4_quantize(P, F16, 2 ** 31 - 1, 257, 257, P, None) == UNSUPPORTED
+
+
+@pytest.mark.parametrize("bad", [dict(rows=0), dict(K=-1), dict(mx=None), dict(mx=P + 4), dict(out=None),
+                                 dict(out=P + 1), dict(type=7)])
+def test_dequantize_refuses(bad):
+    a = dict(mx=P, rows=3, K=100, type=BF16, out=P, stream=None) | bad
+    assert apt.apt_mx4_dequantize(**a) == BAD
+
+
+@pytest.mark.parametrize("bad", [dict(rows=0), dict(K=0), dict(mx=None), dict(mx=P + 4), dict(codes=None),
+                                 dict(scales=None)])
+def test_pack_refuses(bad):
+    a = dict(codes=P, scales=P, rows=3, K=100, mx=P) | bad
+    assert apt.apt_mx4_pack(**a, stream=None) == BAD
+    assert apt.apt_mx4_unpack(a["mx"], a["rows"], a["K"], a["codes"], a["scales"], None) == BAD
+
+
+GEMM = dict(M=5, N=7, K=100, w_mx=P, type=BF16, c=P, workspace=P, workspace_bytes=1 << 30, stream=None)
+COMMON = [dict(M=0), dict(N=0), dict(K=0), dict(M=-1), dict(w_mx=None), dict(w_mx=P + 8), dict(type=0), dict(c=None),
+          dict(c=P + 1), dict(type=F32, c=P + 2)]
+
+
+@pytest.mark.parametrize("bad", COMMON + [dict(a_mx=None), dict(a_mx=P + 1)])
+def test_gemm_refuses(bad):
+    assert apt.apt_mx4_gemm(**(GEMM | dict(a_mx=P) | bad)) == BAD
+
+
+@pytest.mark.parametrize("bad", COMMON + [dict(x=None), dict(x=P + 1), dict(x_type=9), dict(x_stride=99),
+                                          dict(workspace=P + 1)])
+def test_gemm_act_refuses(bad):
+    assert apt.apt_mx4_gemm_act(**(GEMM | dict(x=P, x_type=F16, x_stride=100, M=300) | bad)) == BAD
+
+
+def test_gemm_limits_and_workspace():
+    big = dict(GEMM, K=2 ** 30 + 1)
+    assert apt.apt_mx4_gemm(**(big | dict(a_mx=P))) == UNSUPPORTED
+    assert apt.apt_mx4_gemm_act(**(big | dict(x=P, x_type=F16, x_stride=2 ** 31))) == UNSUPPORTED
+    assert apt.apt_mx4_gemm(**(GEMM | dict(a_mx=P, M=2 ** 31 - 1, N=2 ** 31 - 1))) == UNSUPPORTED
+    for s in ((0, 1, 1), (1, 0, 1), (1, 1, 0), (1, 1, 2 ** 30 + 1)):
+        assert apt.apt_mx4_gemm_workspace_bytes(*s) == 0 and apt.apt_mx4_gemm_act_workspace_bytes(*s) == 0
+    need = apt.apt_mx4_gemm_act_workspace_bytes(300, 7, 100)
+    assert need >= apt.apt_mx4_bytes(300, 100)
+    act = GEMM | dict(M=300, x=P, x_type=F16, x_stride=100)
+    assert apt.apt_mx4_gemm_act(**(act | dict(workspace=None))) == NO_SPACE
+    assert apt.apt_mx4_gemm_act(**(act | dict(workspace_bytes=need - 1))) == NO_SPACE
+
+
+NORM = dict(M=3, K=100, type=BF16, x=P, x_stride=100, residual=P, residual_stride=100, gain=P, eps=1e-5, h=2 * P,
+            y=None, stream=None)
+NORM_BAD = [dict(M=0), dict(K=0), dict(type=F32), dict(type=0), dict(x=None), dict(x=P + 1), dict(x_stride=99),
+            dict(residual=P + 1), dict(residual_stride=99), dict(gain=P + 1), dict(eps=-1e-9), dict(eps=math.nan),
+            dict(eps=math.inf), dict(h=2 * P + 1), dict(y=P + 1), dict(h=P, x_stride=101),
+            dict(x=3 * P, h=P, residual_stride=200)]
+
+
+@pytest.mark.parametrize("bad", NORM_BAD + [dict(q=0), dict(q=9), dict(codes=None), dict(scale=None), dict(scale=P + 1)])
+def test_rmsnorm_codes_refuses(bad):
+    assert apt.apt_rmsnorm_codes(**(NORM | dict(q=8, codes=P, scale=P) | bad)) == BAD
+
+
+@pytest.mark.parametrize("bad", NORM_BAD + [dict(mx=None), dict(mx=P + 8)])
+def test_rmsnorm_mx4_refuses(bad):
+    assert apt.apt_rmsnorm_mx4(**(NORM | dict(mx=P) | bad)) == BAD
+
+
+def test_rmsnorm_limits():
+    big = NORM | dict(K=2 ** 30 + 1, x_stride=2 ** 31, residual_stride=2 ** 31)
+    assert apt.apt_rmsnorm_codes(**(big | dict(q=8, codes=P, scale=P))) == UNSUPPORTED
+    assert apt.apt_rmsnorm_mx4(**(big | dict(mx=P))) == UNSUPPORTED
+
+
+@pytest.mark.parametrize("bad", [dict(M=0), dict(K=0), dict(codes=None), dict(scale=None), dict(scale=P + 1),
+                                 dict(type=0), dict(out=None), dict(out=P + 1)])
+def test_dequantize_codes_refuses(bad):
+    assert apt.apt_dequantize_codes(**(dict(codes=P, scale=P, M=3, K=5, type=F16, out=P, stream=None) | bad)) == BAD
+
+
+def test_helpers_refuse_host_tensors_and_wrong_shapes():
+    x = torch.zeros(2, 64, dtype=torch.float16)
+    w = apt.Mx4(x, 4, 64)
+    for call in (lambda: apt.mx4_quantize(x), lambda: apt.mx4_gemm_act(x, w),
+                 lambda: apt.rmsnorm_codes(x, None, 8, 1e-5), lambda: apt.rmsnorm_mx4(x, None, 1e-5),
+                 lambda: apt.rmsnorm_mx4(x.float(), None, 1e-5), lambda: apt.mx4_gemm(apt.Mx4(x, 2, 32), w),
+                 lambda: apt.mx4_gemm(w, w, torch.int32), lambda: apt.dequantize(x, x),
+                 lambda: apt.mx4_pack(x, x, 64)):
+        with pytest.raises(apt.AptError) as e:
+            call()
+        assert e.value.status == BAD
