@@ -57,8 +57,8 @@ size_t apt_mx4_bytes(int rows, int K);
  *   stride  elements from a row to the next, >= K
  *   mx      device, apt_mx4_bytes(rows, K) bytes, 16-byte aligned
  * Errors: APT_ERR_INVALID_ARG for rows < 1, K < 1, stride < K, an unknown type,
- * NULL or misaligned pointers; APT_ERR_UNSUPPORTED for K > 2^30;
- * APT_ERR_HIP on launch failure. */
+ * NULL or misaligned pointers; APT_ERR_UNSUPPORTED for K > 2^30 or an operand
+ * of more than 2^23 groups x steps (16 GB); APT_ERR_HIP on launch failure. */
 apt_status_t apt_mx4_quantize(const void* x, int type, int rows, int K, int64_t stride, void* mx,
                               void* stream);
 
@@ -89,8 +89,8 @@ apt_status_t apt_mx4_unpack(const void* mx, int rows, int K, uint8_t* codes, uin
  * The result does not depend on what else runs: sums are taken in an order fixed
  * by the sizes.  NaN scales reach only the outputs of their rows.
  * Errors: APT_ERR_INVALID_ARG for sizes < 1, an unknown type, NULL or misaligned
- * pointers; APT_ERR_UNSUPPORTED for K > 2^30 or more than 2^31 - 1 output tiles;
- * APT_ERR_WORKSPACE; APT_ERR_HIP on launch failure. */
+ * pointers; APT_ERR_UNSUPPORTED for K > 2^24, an operand of more than 2^23
+ * groups x steps or an output of more than 2^23 tiles; APT_ERR_WORKSPACE; APT_ERR_HIP on launch failure. */
 size_t apt_mx4_gemm_workspace_bytes(int M, int N, int K);
 apt_status_t apt_mx4_gemm(int M, int N, int K, const void* a_mx, const void* w_mx, int type, void* c,
                           void* workspace, size_t workspace_bytes, void* stream);

@@ -1,72 +1,94 @@
 // mx4_gemm.hip - C = A * W^T of two MX4 operands on the block-scaled MFMA, for
-// gfx950.
-#include "mx4.h"
+// gfx950: the choice among the kernels of mx4_thin.h and mx4_tile.h, and their
+// launches.
+#include <algorithm>
+
+#include "mx4_thin.h"
 
 namespace apt {
 namespace {
 
 using namespace mx4;
 
-constexpr int kWave = 64;
-constexpr int kWaves = 4;
-
-typedef int v8i __attribute__((ext_vector_type(8)));
-typedef float v16f __attribute__((ext_vector_type(16)));
-
-struct GemmParams {
-  int M, N;
-  Operand a, w;
-  uint8_t* c;
-  int tiles_n;  // of 128 columns
+// A tile shape and what a step of 256 elements of K costs a workgroup of it, in
+// us: on its own on a compute unit, and its share of a compute unit's
+// throughput when the whole chip is busy.  Measured at bf16 output from the
+// slopes over K = 2048..8192 of 64, 256 and 2048 rows by 4096 and 11008 columns.
+struct Tile {
+  int mb, nb;
+  double alone, share, fixed;
 };
+constexpr Tile kTiles[] = {
+    {1, 1, 0.28, 0.28, 0.0},  // 32 x 128
+    {2, 1, 0.33, 0.36, 0.0},  // 64 x 128
+    {4, 1, 0.39, 0.58, 0.0},  // 128 x 128
+    {4, 2, 0.52, 0.84, 0.0},  // 128 x 256
+    {8, 2, 0.94, 1.54, 4.0},  // 256 x 256, one workgroup per compute unit: its epilogue stands alone
+};
+constexpr int kNumTiles = sizeof(kTiles) / sizeof(kTiles[0]);
+constexpr double kUnits = 256.0;  // compute units
 
-template <class T>
-__device__ __forceinline__ void store_value(uint8_t* c, int64_t at, float v) {
-  if constexpr (T::kBytes == 4) reinterpret_cast<float*>(c)[at] = v;
-  else reinterpret_cast<uint16_t*>(c)[at] = T::from_float(v);
+int64_t tiles_of(int M, int N, const Tile& t) {
+  return ((int64_t)M + t.mb * 32 - 1) / (t.mb * 32) * (((int64_t)N + t.nb * 128 - 1) / (t.nb * 128));
 }
 
-__device__ __forceinline__ v8i operand_of(u32x4 v) {
-  return v8i{(int)v[0], (int)v[1], (int)v[2], (int)v[3], 0, 0, 0, 0};
+double per_step(double tiles, double alone, double share) {
+  const double load = tiles / kUnits;
+  return std::max(alone, share * (load > 1.0 ? (double)(int64_t)(load + 0.999) : load));
 }
 
-// 32 rows x 128 columns per workgroup, 32 x 32 per wave.
-template <class T>
-__global__ __launch_bounds__(kWave* kWaves) void gemm_kernel(GemmParams p) {
-  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-  const int r = lane % 32, h = lane / 32;
-  const int64_t m0 = (int64_t)(blockIdx.x / (unsigned)p.tiles_n) * 32;
-  const int64_t n0 = (int64_t)(blockIdx.x % (unsigned)p.tiles_n) * 128 + wave * 32;
-  if (n0 >= p.N) return;
-  const int S = p.a.steps;
-  // (rows past the edge read the last group: their outputs are not stored)
-  const int64_t ga = min(m0 / 16 + r / 16, p.a.groups - 1), gw = min(n0 / 16 + r / 16, p.w.groups - 1);
-  const uint8_t* const ac = p.a.codes + ga * S * kCodeBytes + h * 256 + r % 16 * 16;
-  const uint8_t* const wc = p.w.codes + gw * S * kCodeBytes + h * 256 + r % 16 * 16;
-  const uint8_t* const as = p.a.scales + ga * S * kScaleBytes + h * 64 + r % 16 * 4;
-  const uint8_t* const ws = p.w.scales + gw * S * kScaleBytes + h * 64 + r % 16 * 4;
-  v16f acc = {};
-  for (int t = 0; t < S; ++t) {
-    const int sa = *reinterpret_cast<const int*>(as + (int64_t)t * kScaleBytes);
-    const int sw = *reinterpret_cast<const int*>(ws + (int64_t)t * kScaleBytes);
-    u32x4 av[4], wv[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      av[i] = *reinterpret_cast<const u32x4*>(ac + (int64_t)t * kCodeBytes + i * 512);
-      wv[i] = *reinterpret_cast<const u32x4*>(wc + (int64_t)t * kCodeBytes + i * 512);
+// The kernel of a problem: -1 for the few-row kernel, else an index into kTiles.
+// Up to 32 rows the few-row kernel is the faster everywhere (32 x 11008 x 4096
+// 7.2 us against 7.7, 32 x 4096 x 11008 6.8 against 14.7); from 65 on it does not
+// apply; between them the modelled times decide (64 x 11008 x 4096 9.9 against
+// 7.7 us on 32 x 128 tiles, 64 x 4096 x 11008 9.2 against 12.8).  Among the tiles
+// a large one costs fewer loads per MFMA and a small one fills the chip:
+// 2048 x 11008 x 4096 takes 49 us at 128 x 256 and 56, 68, 92 at 128, 64 and 32 x
+// 128; 333 x 5003 x 2999 7.6 us at 64 x 128, 9.1 and 12.7 at 128 x 128 and 128 x
+// 256.  What all of them need besides (launch, first loads, output) is left out.
+int kernel_of(int M, int N, int K) {
+  if (M <= 32) return -1;
+  const double S = steps(K);
+  int best = -1;
+  double least = M <= kThinRows ? S * std::max(0.17, 0.12 * (double)groups(N) / kUnits) - 1.5 : 1e30;
+  for (int i = 0; i < kNumTiles; ++i) {
+    const Tile& t = kTiles[i];
+    const double us = S * per_step((double)tiles_of(M, N, t), t.alone, t.share) + t.fixed;
+    if (us < least) {
+      least = us;
+      best = i;
     }
-    acc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand_of(wv[0]), operand_of(av[0]), acc, 4, 4, 0, sw, 0, sa);
-    acc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand_of(wv[1]), operand_of(av[1]), acc, 4, 4, 1, sw, 1, sa);
-    acc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand_of(wv[2]), operand_of(av[2]), acc, 4, 4, 2, sw, 2, sa);
-    acc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand_of(wv[3]), operand_of(av[3]), acc, 4, 4, 3, sw, 3, sa);
   }
-  const int64_t m = m0 + r;
-  if (m >= p.M) return;
-#pragma unroll
-  for (int v = 0; v < 16; ++v) {
-    const int64_t n = n0 + v / 4 * 8 + h * 4 + v % 4;
-    if (n < p.N) store_value<T>(p.c, m * p.N + n, acc[v]);
+  return best;
+}
+
+template <class T, int I>
+hipError_t launch_tile(GemmParams p, hipStream_t s) {
+  constexpr int MB = kTiles[I].mb, NB = kTiles[I].nb;
+  // (registers: four steps of weights where the accumulators leave room)
+  constexpr int WD = NB == 1 ? 4 : 2;
+  p.tiles_m = (int)(((int64_t)p.M + MB * 32 - 1) / (MB * 32));
+  p.tiles_n = (int)(((int64_t)p.N + NB * 128 - 1) / (NB * 128));
+  const dim3 grid((unsigned)(p.tiles_m * p.tiles_n)), block(kWave * kTileWaves);
+  return launch_kernel(tile_kernel<T, MB, NB, WD>, grid, block, 0, s, p);
+}
+
+template <class T>
+hipError_t launch_tile_of(const GemmParams& p, int kernel, hipStream_t s) {
+  switch (kernel) {
+    case 0: return launch_tile<T, 0>(p, s);
+    case 1: return launch_tile<T, 1>(p, s);
+    case 2: return launch_tile<T, 2>(p, s);
+    case 3: return launch_tile<T, 3>(p, s);
+    default: return launch_tile<T, 4>(p, s);
   }
+}
+
+hipError_t launch_thin(const ThinParams& p, hipStream_t s) {
+  const dim3 grid((unsigned)p.w.groups), block(kWave * kThinWaves);
+  if (p.M <= 16) return launch_kernel(thin_kernel<1>, grid, block, 0, s, p);
+  if (p.M <= 32) return launch_kernel(thin_kernel<2>, grid, block, 0, s, p);
+  return launch_kernel(thin_kernel<4>, grid, block, 0, s, p);
 }
 
 }  // namespace
@@ -74,8 +96,8 @@ __global__ __launch_bounds__(kWave* kWaves) void gemm_kernel(GemmParams p) {
 namespace mx4 {
 
 int64_t gemm_tiles(int M, int N, int K) {
-  (void)K;
-  return ((int64_t)M + 31) / 32 * (((int64_t)N + 127) / 128);
+  const int k = kernel_of(M, N, K);
+  return k < 0 ? groups(N) : tiles_of(M, N, kTiles[k]);
 }
 
 size_t gemm_workspace(int M, int N, int K) {
@@ -86,12 +108,13 @@ size_t gemm_workspace(int M, int N, int K) {
 hipError_t launch_gemm(int M, int N, int K, const Operand& a, const Operand& w, int type, void* c, void* workspace,
                        hipStream_t s) {
   (void)workspace;
-  GemmParams p{M, N, a, w, static_cast<uint8_t*>(c), (int)(((int64_t)N + 127) / 128)};
-  const dim3 grid((unsigned)gemm_tiles(M, N, K)), block(kWave * kWaves);
+  const int k = kernel_of(M, N, K);
+  if (k < 0) return launch_thin(ThinParams{M, N, type, a, w, static_cast<uint8_t*>(c)}, s);
+  const GemmParams p{M, N, a, w, static_cast<uint8_t*>(c), 0, 0};
   switch (type) {
-    case APT_TYPE_FP16: return launch_kernel(gemm_kernel<Half>, grid, block, 0, s, p);
-    case APT_TYPE_BF16: return launch_kernel(gemm_kernel<Bf16>, grid, block, 0, s, p);
-    default: return launch_kernel(gemm_kernel<Float>, grid, block, 0, s, p);
+    case APT_TYPE_FP16: return launch_tile_of<Half>(p, k, s);
+    case APT_TYPE_BF16: return launch_tile_of<Bf16>(p, k, s);
+    default: return launch_tile_of<Float>(p, k, s);
   }
 }
 

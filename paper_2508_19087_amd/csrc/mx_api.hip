@@ -9,10 +9,11 @@ namespace {
 
 using apt::hip_status;
 
-constexpr int kMaxK = 1 << 30;  // rows are indexed with 32-bit ints
-// Group-steps of an operand: a launch takes up to 128 threads for each and
-// holds fewer than 2^32 (64 GB of codes).
-constexpr int64_t kMaxUnits = (int64_t)1 << 24;
+constexpr int kMaxK = 1 << 30;         // rows are indexed with 32-bit ints
+constexpr int kMaxProductK = 1 << 24;  // a tile's operands are addressed with 32-bit offsets
+// Group-steps of an operand (16 GB of codes) and tiles of a product: a launch
+// takes up to 256 threads for each and holds fewer than 2^32.
+constexpr int64_t kMaxUnits = (int64_t)1 << 23;
 
 bool type_ok(int t) { return t == APT_TYPE_FP16 || t == APT_TYPE_BF16 || t == APT_TYPE_FP32; }
 bool aligned(const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
@@ -35,7 +36,7 @@ apt_status_t product_check(int M, int N, int K, const void* w_mx, int type, cons
   const apt_status_t st = operand_check(N, K, w_mx);
   if (M < 1 || st == APT_ERR_INVALID_ARG || !type_ok(type) || c == nullptr || !aligned(c, type_bytes(type)))
     return APT_ERR_INVALID_ARG;
-  if (st != APT_OK || K > kMaxK || apt::mx4::groups(M) * apt::mx4::steps(K) > kMaxUnits ||
+  if (st != APT_OK || K > kMaxProductK || apt::mx4::groups(M) * apt::mx4::steps(K) > kMaxUnits ||
       apt::mx4::gemm_tiles(M, N, K) > kMaxUnits)
     return APT_ERR_UNSUPPORTED;
   return APT_OK;
@@ -51,7 +52,7 @@ size_t align256(size_t x) { return (x + 255) / 256 * 256; }
 
 // Sizes of a product that an entry point takes.
 bool sizes_ok(int M, int N, int K) {
-  return M >= 1 && N >= 1 && K >= 1 && K <= kMaxK && apt::mx4::groups(M) * apt::mx4::steps(K) <= kMaxUnits &&
+  return M >= 1 && N >= 1 && K >= 1 && K <= kMaxProductK && apt::mx4::groups(M) * apt::mx4::steps(K) <= kMaxUnits &&
          apt::mx4::groups(N) * apt::mx4::steps(K) <= kMaxUnits && apt::mx4::gemm_tiles(M, N, K) <= kMaxUnits;
 }
 

@@ -180,7 +180,9 @@ def test_gemm(M, N, K, kind):
     check_product(got, ref.values(*a), ref.values(*w), K, kind, str((M, N, K)))
 
 
-@pytest.mark.parametrize("M,N,K", GEMM + [(1, 11008, 4096), (8, 4096, 11008), (1024, 1024, 1024), (2100, 300, 512)])
+@pytest.mark.parametrize("M,N,K", GEMM + [(1, 11008, 4096), (8, 4096, 11008), (1024, 1024, 1024), (2100, 300, 512),
+                                          (64, 2048, 11008), (1024, 4096, 11008), (500, 1000, 1500), (768, 2048, 1800),
+                                          (2048, 4096, 2300), (4096, 4096, 1100)])
 def test_gemm_is_exact_where_sums_fit(M, N, K):
     """Scales of 1 or 2: every partial sum is a multiple of 1/4 below 2^22 (36 * 4 * 11008 < 2^21), so fp32 holds it."""
     a, w = random_mx4(M, M, K, 127, 129), random_mx4(N, N, K, 127, 129)
