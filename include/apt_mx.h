@@ -83,24 +83,26 @@ apt_status_t apt_mx4_unpack(const void* mx, int rows, int K, uint8_t* codes, uin
  * sums and one rounding (to nearest even) to the output's type.
  *   a_mx, w_mx  device, MX4 operands of M and N rows of K values
  *   type, c     output type and device [M][N] row-major, aligned to its element size
- *   workspace, workspace_bytes  device scratch of at least
- *               apt_mx4_gemm_workspace_bytes(M, N, K) bytes, 16-byte aligned
- *               (NULL when 0); overwritten; calls sharing it must not overlap in time
  * The result does not depend on what else runs: sums are taken in an order fixed
  * by the sizes.  NaN scales reach only the outputs of their rows.
  * Errors: APT_ERR_INVALID_ARG for sizes < 1, an unknown type, NULL or misaligned
  * pointers; APT_ERR_UNSUPPORTED for K > 2^24, an operand of more than 2^23
- * groups x steps or an output of more than 2^23 tiles; APT_ERR_WORKSPACE; APT_ERR_HIP on launch failure. */
-size_t apt_mx4_gemm_workspace_bytes(int M, int N, int K);
+ * groups x steps or an output of more than 2^23 tiles; APT_ERR_HIP on launch
+ * failure. */
 apt_status_t apt_mx4_gemm(int M, int N, int K, const void* a_mx, const void* w_mx, int type, void* c,
-                          void* workspace, size_t workspace_bytes, void* stream);
+                          void* stream);
 
 /* C = A * W^T with the activations given unpacked and quantized inside the call
  * as apt_mx4_quantize does; the result equals that of apt_mx4_quantize followed
- * by apt_mx4_gemm, bit for bit.
+ * by apt_mx4_gemm, bit for bit.  Up to 16 rows of together 16384 elements (rows
+ * padded to 256) are quantized by the product's kernel itself; others go through
+ * the workspace.
  *   x, x_type, x_stride  as apt_mx4_quantize, M rows
- *   workspace  apt_mx4_gemm_act_workspace_bytes(M, N, K) bytes
- * Errors as apt_mx4_quantize and apt_mx4_gemm. */
+ *   workspace, workspace_bytes  device scratch of at least
+ *               apt_mx4_gemm_act_workspace_bytes(M, N, K) bytes, 16-byte aligned
+ *               (NULL when 0); overwritten; calls sharing it must not overlap in time
+ * Errors as apt_mx4_quantize and apt_mx4_gemm, and APT_ERR_WORKSPACE when the
+ * workspace is missing or too small. */
 size_t apt_mx4_gemm_act_workspace_bytes(int M, int N, int K);
 apt_status_t apt_mx4_gemm_act(int M, int N, int K, const void* x, int x_type, int64_t x_stride,
                               const void* w_mx, int type, void* c, void* workspace,

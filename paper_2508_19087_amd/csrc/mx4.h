@@ -162,12 +162,14 @@ hipError_t launch_rmsnorm(int M, int K, int type, const void* x, int64_t x_strid
                           const Operand* mx, hipStream_t s);
 hipError_t launch_dequantize_codes(const int8_t* codes, const uint16_t* scale, int M, int K, int type, void* out,
                                    hipStream_t s);
-// The product of two operands (mx4_gemm.hip); `tiles` the output tiles of the
+// The product of two operands (mx4_gemm.hip); gemm_tiles: the workgroups of the
 // launch, for the ABI's bound.
 int64_t gemm_tiles(int M, int N, int K);
-size_t gemm_workspace(int M, int N, int K);
-hipError_t launch_gemm(int M, int N, int K, const Operand& a, const Operand& w, int type, void* c, void* workspace,
-                       hipStream_t s);
+hipError_t launch_gemm(int M, int N, int K, const Operand& a, const Operand& w, int type, void* c, hipStream_t s);
+// The same from rows, quantized in the product's kernel, where gemm_takes_rows.
+bool gemm_takes_rows(int M, int K);
+hipError_t launch_gemm_rows(int M, int N, int K, const void* x, int x_type, int64_t x_stride, const Operand& w, int type,
+                            void* c, hipStream_t s);
 
 }  // namespace mx4
 }  // namespace apt

@@ -28,6 +28,14 @@ constexpr Tile kTiles[] = {
 constexpr int kNumTiles = sizeof(kTiles) / sizeof(kTiles[0]);
 constexpr double kUnits = 256.0;  // compute units
 
+// Activations given as rows are quantized by the few-row kernel's workgroups
+// themselves, each on its own, up to this many elements (rows padded to steps).
+// One row of 4096 to 11008 columns: 6.1 us in a graph against 8.8 with a launch
+// before; the conversion then adds about 1 us per 4096 elements, so that 4 rows
+// of 4096 break even in a graph (9.6 against 8.9 us with 11008 columns, 5.7 and
+// 5.7 with 4096) and save a launch's 2 us of host time in a call by itself.
+constexpr int64_t kFusedElements = 16384;
+
 int64_t tiles_of(int M, int N, const Tile& t) {
   return ((int64_t)M + t.mb * 32 - 1) / (t.mb * 32) * (((int64_t)N + t.nb * 128 - 1) / (t.nb * 128));
 }
@@ -86,9 +94,9 @@ hipError_t launch_tile_of(const GemmParams& p, int kernel, hipStream_t s) {
 
 hipError_t launch_thin(const ThinParams& p, hipStream_t s) {
   const dim3 grid((unsigned)p.w.groups), block(kWave * kThinWaves);
-  if (p.M <= 16) return launch_kernel(thin_kernel<1>, grid, block, 0, s, p);
-  if (p.M <= 32) return launch_kernel(thin_kernel<2>, grid, block, 0, s, p);
-  return launch_kernel(thin_kernel<4>, grid, block, 0, s, p);
+  if (p.M <= 16) return launch_kernel(thin_kernel<1, void>, grid, block, 0, s, p);
+  if (p.M <= 32) return launch_kernel(thin_kernel<2, void>, grid, block, 0, s, p);
+  return launch_kernel(thin_kernel<4, void>, grid, block, 0, s, p);
 }
 
 }  // namespace
@@ -100,21 +108,28 @@ int64_t gemm_tiles(int M, int N, int K) {
   return k < 0 ? groups(N) : tiles_of(M, N, kTiles[k]);
 }
 
-size_t gemm_workspace(int M, int N, int K) {
-  (void)M, (void)N, (void)K;
-  return 0;
-}
-
-hipError_t launch_gemm(int M, int N, int K, const Operand& a, const Operand& w, int type, void* c, void* workspace,
-                       hipStream_t s) {
-  (void)workspace;
+hipError_t launch_gemm(int M, int N, int K, const Operand& a, const Operand& w, int type, void* c, hipStream_t s) {
   const int k = kernel_of(M, N, K);
-  if (k < 0) return launch_thin(ThinParams{M, N, type, a, w, static_cast<uint8_t*>(c)}, s);
+  if (k < 0) return launch_thin(ThinParams{M, N, type, w.steps, a, w, static_cast<uint8_t*>(c), nullptr, 0, K}, s);
   const GemmParams p{M, N, a, w, static_cast<uint8_t*>(c), 0, 0};
   switch (type) {
     case APT_TYPE_FP16: return launch_tile_of<Half>(p, k, s);
     case APT_TYPE_BF16: return launch_tile_of<Bf16>(p, k, s);
     default: return launch_tile_of<Float>(p, k, s);
+  }
+}
+
+bool gemm_takes_rows(int M, int K) { return M <= 16 && (int64_t)M * steps(K) * kStep <= kFusedElements; }
+
+hipError_t launch_gemm_rows(int M, int N, int K, const void* x, int x_type, int64_t x_stride, const Operand& w, int type,
+                            void* c, hipStream_t s) {
+  const ThinParams p{M, N, type, w.steps, Operand{}, w, static_cast<uint8_t*>(c), static_cast<const uint8_t*>(x), x_stride, K};
+  const dim3 grid((unsigned)w.groups), block(kWave * kThinWaves);
+  const size_t lds = thin_lds_bytes(M, K);
+  switch (x_type) {
+    case APT_TYPE_FP16: return launch_kernel(thin_kernel<1, Half>, grid, block, lds, s, p);
+    case APT_TYPE_BF16: return launch_kernel(thin_kernel<1, Bf16>, grid, block, lds, s, p);
+    default: return launch_kernel(thin_kernel<1, Float>, grid, block, lds, s, p);
   }
 }
 

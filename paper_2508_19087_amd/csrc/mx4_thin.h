@@ -37,8 +37,13 @@ __device__ __forceinline__ void lds_barrier() {
 
 struct ThinParams {
   int M, N, type;
-  Operand a, w;
+  int steps;
+  Operand a, w;       // a: unused with rows
   uint8_t* c;
+  // activations as rows (thin_kernel of an element type)
+  const uint8_t* x;
+  int64_t x_stride;   // elements
+  int K;
 };
 
 __device__ __forceinline__ void store_output(uint8_t* c, int type, int64_t at, float v) {
@@ -46,29 +51,69 @@ __device__ __forceinline__ void store_output(uint8_t* c, int type, int64_t at, f
   else reinterpret_cast<uint16_t*>(c)[at] = type == APT_TYPE_FP16 ? Half::from_float(v) : Bf16::from_float(v);
 }
 
-// MT: groups of 16 activation rows.
-template <int MT>
+// Rows quantized into LDS by a workgroup: the 16 bytes of block b of step t of
+// row m at ((t * 8 + b) * M + m) * 16, behind them the scale dword of half h at
+// ((t * 2 + h) * M + m) * 4.
+inline size_t thin_lds_bytes(int M, int K) { return (size_t)steps(K) * M * (kStep / 2 + kStep / kBlock); }
+
+// A thread's share of them: groups of eight elements, four neighbouring lanes to
+// a block, kHeld at a time.  load() issues the first loads of a batch and
+// store() converts it.
+template <class X>
+struct RowShare {
+  static constexpr int kHeld = 2, kPieces = 8 / X::kVec;
+  u32x4 v[kHeld][kPieces];
+
+  __device__ __forceinline__ void load(const ThinParams& p, int i0) {
+    const int per_row = p.steps * (kStep / 8), all = per_row * p.M;
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) {
+      const int x = min(i0 + i * kThinWaves * kWave, all - 1);
+      const int m = x / per_row, k = (x - m * per_row) * 8;
+      const uint8_t* const row = p.x + m * p.x_stride * X::kBytes;
+#pragma unroll
+      for (int j = 0; j < kPieces; ++j) v[i][j] = load_vector<X>(row, k + j * X::kVec, p.K);
+    }
+  }
+  __device__ __forceinline__ void store(const ThinParams& p, uint8_t* lds, int i0) const {
+    const int per_row = p.steps * (kStep / 8), all = per_row * p.M;
+    uint8_t* const scales = lds + p.steps * p.M * (kStep / 2);
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) {
+      const int x = i0 + i * kThinWaves * kWave;
+      uint32_t m = 0u;
+#pragma unroll
+      for (int j = 0; j < kPieces; ++j) m = fold_magnitude<X>(m, v[i][j]);
+      m = widest<X>(m);
+      m = max(m, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0xB1, 0xF, 0xF, false));  // lane ^ 1
+      m = max(m, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0x4E, 0xF, 0xF, false));  // lane ^ 2
+      const uint32_t byte = scale_byte<X>(m);
+      const uint32_t c = byte == 255u ? 0u : codes_of<X>(v[i], scale_of(byte));
+      if (x >= all) continue;
+      const int row = x / per_row, y = x - row * per_row;  // eighth y of the row
+      const int block = y / 4;
+      *reinterpret_cast<uint32_t*>(lds + (block * p.M + row) * 16 + y % 4 * 4) = c;
+      if (y % 4 == 0) scales[((block / 8 * 2 + block % 2) * p.M + row) * 4 + block % 8 / 2] = (uint8_t)byte;
+    }
+  }
+};
+
+// MT: groups of 16 activation rows.  X: void for an operand, or the element type
+// of the rows that the workgroup quantizes into LDS itself (MT = 1).
+template <int MT, class X>
 __global__ __launch_bounds__(kThinWaves* kWave) void thin_kernel(ThinParams p) {
   constexpr int KW = kThinWaves;
+  constexpr bool kRows = !std::is_void<X>::value;
+  extern __shared__ __attribute__((aligned(16))) uint8_t rows_lds[];
   __shared__ float sums[KW][MT * 256];
   const int lane = threadIdx.x % kWave;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int s = lane % 16, q = lane / 16;
-  const int S = p.a.steps;
+  const int S = p.steps;
   const int64_t g = blockIdx.x;  // weight row group
   const uint8_t* const wc = p.w.codes + g * S * kCodeBytes + lane * 16;
   const uint8_t* const ws = p.w.scales + g * S * kScaleBytes + q % 2 * 64 + s * 4;
   const int shift = q / 2 * 8;
-
-  // (rows that are not there read the last one: their sums are not stored)
-  const uint8_t* ac[MT];
-  const uint8_t* as[MT];
-#pragma unroll
-  for (int i = 0; i < MT; ++i) {
-    const int m = min(i * 16 + s, p.M - 1);
-    ac[i] = p.a.codes + (int64_t)(m / 16) * S * kCodeBytes + q * 256 + m % 16 * 16;
-    as[i] = p.a.scales + (int64_t)(m / 16) * S * kScaleBytes + q % 2 * 64 + m % 16 * 4;
-  }
 
   v4f acc[MT];
 #pragma unroll
@@ -82,18 +127,53 @@ __global__ __launch_bounds__(kThinWaves* kWave) void thin_kernel(ThinParams p) {
     w[u][1] = *reinterpret_cast<const u32x4*>(wc + at * kCodeBytes + 1024);
     sw[u] = *reinterpret_cast<const uint32_t*>(ws + at * kScaleBytes);
   };
+  // (rows that are not there read the last one: their sums are not stored)
+  const uint8_t* ac[MT];
+  const uint8_t* as[MT];
+#pragma unroll
+  for (int i = 0; i < MT; ++i) {
+    const int m = min(i * 16 + s, p.M - 1);
+    if constexpr (kRows) {
+      ac[i] = rows_lds + (q * p.M + m) * 16;
+      as[i] = rows_lds + S * p.M * (kStep / 2) + (q % 2 * p.M + m) * 4;
+    } else {
+      ac[i] = p.a.codes + (int64_t)(m / 16) * S * kCodeBytes + q * 256 + m % 16 * 16;
+      as[i] = p.a.scales + (int64_t)(m / 16) * S * kScaleBytes + q % 2 * 64 + m % 16 * 4;
+    }
+  }
+  const int64_t a_step = kRows ? p.M * (kStep / 2) : kCodeBytes, as_step = kRows ? p.M * (kStep / kBlock) : kScaleBytes;
+  const int a_half = kRows ? p.M * (kStep / 4) : 1024;
   auto load_a = [&](int u, int t) __attribute__((always_inline)) {
     const int64_t at = min(t, S - 1);
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
-      a[u][i][0] = *reinterpret_cast<const u32x4*>(ac[i] + at * kCodeBytes);
-      a[u][i][1] = *reinterpret_cast<const u32x4*>(ac[i] + at * kCodeBytes + 1024);
-      sa[u][i] = *reinterpret_cast<const uint32_t*>(as[i] + at * kScaleBytes);
+      a[u][i][0] = *reinterpret_cast<const u32x4*>(ac[i] + at * a_step);
+      a[u][i][1] = *reinterpret_cast<const u32x4*>(ac[i] + at * a_step + a_half);
+      sa[u][i] = *reinterpret_cast<const uint32_t*>(as[i] + at * as_step);
     }
   };
-  load_a(0, wave);
+  if constexpr (kRows) {
+    // the rows' loads leave before the weights', whose arrival then overlaps the
+    // conversion (loads return in order)
+    RowShare<X> share;
+    share.load(p, threadIdx.x);
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-  for (int u = 0; u < kAhead; ++u) load_w(u, wave + u * KW);
+    for (int u = 0; u < kAhead; ++u) load_w(u, wave + u * KW);
+    __builtin_amdgcn_sched_barrier(0);
+    share.store(p, rows_lds, threadIdx.x);
+    const int all = S * (kStep / 8) * p.M;
+    for (int i = RowShare<X>::kHeld * KW * kWave; i < all; i += RowShare<X>::kHeld * KW * kWave) {
+      share.load(p, i + threadIdx.x);
+      share.store(p, rows_lds, i + threadIdx.x);
+    }
+    lds_barrier();
+    load_a(0, wave);
+  } else {
+    load_a(0, wave);
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) load_w(u, wave + u * KW);
+  }
   auto multiply = [&](int u) __attribute__((always_inline)) {
     const int x = (int)(sw[u] >> shift);
 #pragma unroll

@@ -42,14 +42,6 @@ apt_status_t product_check(int M, int N, int K, const void* w_mx, int type, cons
   return APT_OK;
 }
 
-apt_status_t workspace_check(size_t need, const void* workspace, size_t bytes) {
-  if (need == 0) return APT_OK;
-  if (workspace == nullptr || bytes < need) return APT_ERR_WORKSPACE;
-  return aligned(workspace, 16) ? APT_OK : APT_ERR_INVALID_ARG;
-}
-
-size_t align256(size_t x) { return (x + 255) / 256 * 256; }
-
 // Sizes of a product that an entry point takes.
 bool sizes_ok(int M, int N, int K) {
   return M >= 1 && N >= 1 && K >= 1 && K <= kMaxProductK && apt::mx4::groups(M) * apt::mx4::steps(K) <= kMaxUnits &&
@@ -109,24 +101,17 @@ apt_status_t apt_mx4_unpack(const void* mx, int rows, int K, uint8_t* codes, uin
                                             static_cast<hipStream_t>(stream)));
 }
 
-size_t apt_mx4_gemm_workspace_bytes(int M, int N, int K) {
-  return sizes_ok(M, N, K) ? apt::mx4::gemm_workspace(M, N, K) : 0;
-}
-
-apt_status_t apt_mx4_gemm(int M, int N, int K, const void* a_mx, const void* w_mx, int type, void* c, void* workspace,
-                          size_t workspace_bytes, void* stream) {
+apt_status_t apt_mx4_gemm(int M, int N, int K, const void* a_mx, const void* w_mx, int type, void* c, void* stream) {
   const apt_status_t st = product_check(M, N, K, w_mx, type, c);
   if (st == APT_ERR_INVALID_ARG || a_mx == nullptr || !aligned(a_mx, 16)) return APT_ERR_INVALID_ARG;
   if (st != APT_OK) return st;
-  const apt_status_t ws = workspace_check(apt::mx4::gemm_workspace(M, N, K), workspace, workspace_bytes);
-  if (ws != APT_OK) return ws;
   return hip_status(apt::mx4::launch_gemm(M, N, K, apt::mx4::operand(a_mx, M, K), apt::mx4::operand(w_mx, N, K), type, c,
-                                          workspace, static_cast<hipStream_t>(stream)));
+                                          static_cast<hipStream_t>(stream)));
 }
 
 size_t apt_mx4_gemm_act_workspace_bytes(int M, int N, int K) {
-  if (!sizes_ok(M, N, K)) return 0;
-  return align256(apt::mx4::gemm_workspace(M, N, K)) + apt::mx4::operand_bytes(M, K);
+  if (!sizes_ok(M, N, K) || apt::mx4::gemm_takes_rows(M, K)) return 0;
+  return apt::mx4::operand_bytes(M, K);
 }
 
 apt_status_t apt_mx4_gemm_act(int M, int N, int K, const void* x, int x_type, int64_t x_stride, const void* w_mx,
@@ -134,15 +119,16 @@ apt_status_t apt_mx4_gemm_act(int M, int N, int K, const void* x, int x_type, in
   const apt_status_t st = product_check(M, N, K, w_mx, type, c);
   if (st == APT_ERR_INVALID_ARG || !rows_ok(x, x_type, K, x_stride)) return APT_ERR_INVALID_ARG;
   if (st != APT_OK) return st;
-  const apt_status_t ws = workspace_check(apt_mx4_gemm_act_workspace_bytes(M, N, K), workspace, workspace_bytes);
-  if (ws != APT_OK) return ws;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  // the product's scratch, then the quantized activations
-  const apt::mx4::Operand a = apt::mx4::operand(
-      static_cast<uint8_t*>(workspace) + align256(apt::mx4::gemm_workspace(M, N, K)), M, K);
+  const apt::mx4::Operand w = apt::mx4::operand(w_mx, N, K);
+  const size_t need = apt_mx4_gemm_act_workspace_bytes(M, N, K);
+  if (need == 0) return hip_status(apt::mx4::launch_gemm_rows(M, N, K, x, x_type, x_stride, w, type, c, s));
+  if (workspace == nullptr || workspace_bytes < need) return APT_ERR_WORKSPACE;
+  if (!aligned(workspace, 16)) return APT_ERR_INVALID_ARG;
+  const apt::mx4::Operand a = apt::mx4::operand(workspace, M, K);
   const hipError_t e = apt::mx4::launch_quantize(x, x_type, M, K, x_stride, a, s);
   if (e != hipSuccess) return hip_status(e);
-  return hip_status(apt::mx4::launch_gemm(M, N, K, a, apt::mx4::operand(w_mx, N, K), type, c, workspace, s));
+  return hip_status(apt::mx4::launch_gemm(M, N, K, a, w, type, c, s));
 }
 
 apt_status_t apt_rmsnorm_codes(int M, int K, int type, const void* x, int64_t x_stride, const void* residual,

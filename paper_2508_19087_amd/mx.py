@@ -30,8 +30,7 @@ _SIGNATURES = {
     "apt_mx4_dequantize": (_int, [_vp, _int, _int, _int, _vp, _vp]),
     "apt_mx4_pack": (_int, [_vp, _vp, _int, _int, _vp, _vp]),
     "apt_mx4_unpack": (_int, [_vp, _int, _int, _vp, _vp, _vp]),
-    "apt_mx4_gemm_workspace_bytes": (_size, [_int, _int, _int]),
-    "apt_mx4_gemm": (_int, [_int, _int, _int, _vp, _vp, _int, _vp, _vp, _size, _vp]),
+    "apt_mx4_gemm": (_int, [_int, _int, _int, _vp, _vp, _int, _vp, _vp]),
     "apt_mx4_gemm_act_workspace_bytes": (_size, [_int, _int, _int]),
     "apt_mx4_gemm_act": (_int, [_int, _int, _int, _vp, _int, _i64, _vp, _int, _vp, _vp, _size, _vp]),
     "apt_rmsnorm_codes": (_int, [_int, _int, _int, _vp, _i64, _vp, _i64, _vp, ctypes.c_double, _int, _vp, _vp, _vp,
@@ -81,12 +80,8 @@ def apt_mx4_unpack(mx, rows, K, codes, scales, stream) -> int:
     return lib().apt_mx4_unpack(mx, rows, K, codes, scales, stream)
 
 
-def apt_mx4_gemm_workspace_bytes(M, N, K) -> int:
-    return int(lib().apt_mx4_gemm_workspace_bytes(M, N, K))
-
-
-def apt_mx4_gemm(M, N, K, a_mx, w_mx, type, c, workspace, workspace_bytes, stream) -> int:
-    return lib().apt_mx4_gemm(M, N, K, a_mx, w_mx, type, c, workspace, workspace_bytes, stream)
+def apt_mx4_gemm(M, N, K, a_mx, w_mx, type, c, stream) -> int:
+    return lib().apt_mx4_gemm(M, N, K, a_mx, w_mx, type, c, stream)
 
 
 def apt_mx4_gemm_act_workspace_bytes(M, N, K) -> int:
@@ -112,6 +107,11 @@ def apt_dequantize_codes(codes, scale, M, K, type, out, stream) -> int:
 
 
 # ---- torch helpers (checks, allocation, pointers) -------------------------------
+#
+# A small call's time is the host's (a launch 3.3 us, each allocation 1.2 to 1.7),
+# so these keep to what a call needs: the C functions are called without the
+# wrappers above, new tensors are made like given ones, and devices are compared
+# by index.
 
 _types = None
 
@@ -128,30 +128,56 @@ def _type(dtype, where):
     return t
 
 
-def _require(ok, where, what):
-    if not ok:
-        raise AptError(APT_ERR_INVALID_ARG, "%s: %s" % (where, what))
+def _refuse(where, what):
+    raise AptError(APT_ERR_INVALID_ARG, "%s: %s" % (where, what))
 
 
-def _call(fn, device, stream, args):
-    """fn(*args, raw stream) on `device`."""
+def _call(name, device, stream, *args):
+    """The C function `name` of the arguments and the raw stream, on `device`."""
     C = _torch()._C
-    if stream is not None:
-        _require(stream.device == device, fn.__name__, "a stream of another device")
-        raw = stream.cuda_stream
+    index = device.index
+    if stream is None:
+        raw = C._cuda_getCurrentRawStream(index)
     else:
-        raw = C._cuda_getCurrentRawStream(device.index)
-    if C._cuda_getDevice() == device.index:
-        check(fn(*args, raw), fn.__name__)
+        if stream.device != device:
+            _refuse(name, "a stream of another device")
+        raw = stream.cuda_stream
+    f = getattr(_lib or lib(), name)
+    if C._cuda_getDevice() == index:
+        status = f(*args, raw)
     else:
         with _torch().cuda.device(device):
-            check(fn(*args, raw), fn.__name__)
+            status = f(*args, raw)
+    if status:
+        check(status, name)
+
+
+def _new(like, shape, dtype, stream):
+    """A new tensor on the device of `like`, of the call's stream."""
+    if stream is None:
+        return like.new_empty(shape, dtype=dtype)
+    with _on_stream(stream):
+        return like.new_empty(shape, dtype=dtype)
+
+
+def _new_like(x, dtype, stream):
+    """A new contiguous tensor of x's shape, of the call's stream."""
+    torch = _torch()
+    if stream is None:
+        if x.is_contiguous():
+            return torch.empty_like(x, dtype=dtype)
+        return x.new_empty(x.shape, dtype=dtype)
+    with _on_stream(stream):
+        return x.new_empty(x.shape, dtype=dtype)
 
 
 def _rows(x, where, stream):
     """x, or a copy (made on the call's stream), as rows of adjacent elements, and the stride of its rows."""
-    _require(x.is_cuda and x.dim() == 2, where, "a CUDA tensor of two dimensions is wanted")
+    if not x.is_cuda or x.dim() != 2:
+        _refuse(where, "a CUDA tensor of two dimensions is wanted")
     M, K = x.shape
+    if x.is_contiguous():
+        return x, K
     if (x.stride(1) == 1 or K == 1) and (x.stride(0) >= K or M == 1):
         return x, (x.stride(0) if M > 1 else K)
     with _on_stream(stream):
@@ -166,11 +192,12 @@ class Mx4:
     K: int
 
 
-def _new_mx4(rows, K, device, stream, where) -> Mx4:
-    n = apt_mx4_bytes(rows, K)
-    _require(n > 0, where, "%d rows of %d values" % (rows, K))
-    with _on_stream(stream):
-        return Mx4(_torch().empty(n, dtype=_torch().uint8, device=device), rows, K)
+def _new_mx4(rows, K, like, stream, where) -> Mx4:
+    """An operand on the device of `like`."""
+    n = (_lib or lib()).apt_mx4_bytes(rows, K)
+    if n == 0:
+        _refuse(where, "%d rows of %d values" % (rows, K))
+    return Mx4(_new(like, n, _torch().uint8, stream), rows, K)
 
 
 def mx4_quantize(x, stream=None) -> Mx4:
@@ -178,19 +205,18 @@ def mx4_quantize(x, stream=None) -> Mx4:
     x, stride = _rows(x, "mx4_quantize", stream)
     M, K = x.shape
     t = _type(x.dtype, "mx4_quantize")
-    out = _new_mx4(M, K, x.device, stream, "mx4_quantize")
-    _call(apt_mx4_quantize, x.device, stream, (x.data_ptr(), t, M, K, stride, out.data.data_ptr()))
+    out = _new_mx4(M, K, x, stream, "mx4_quantize")
+    _call("apt_mx4_quantize", x.device, stream, x.data_ptr(), t, M, K, stride, out.data.data_ptr())
     return out
 
 
 def mx4_dequantize(a: Mx4, dtype=None, stream=None):
     """The values of an MX4 operand, [rows][K] of `dtype` (by default bf16, which holds them all)."""
-    torch = _torch()
-    dtype = torch.bfloat16 if dtype is None else dtype
+    dtype = _torch().bfloat16 if dtype is None else dtype
     t = _type(dtype, "mx4_dequantize")
-    with _on_stream(stream):
-        out = torch.empty((a.rows, a.K), dtype=dtype, device=a.data.device)
-    _call(apt_mx4_dequantize, a.data.device, stream, (a.data.data_ptr(), a.rows, a.K, t, out.data_ptr()))
+    data = a.data
+    out = _new(data, (a.rows, a.K), dtype, stream)
+    _call("apt_mx4_dequantize", data.device, stream, data.data_ptr(), a.rows, a.K, t, out.data_ptr())
     return out
 
 
@@ -198,52 +224,36 @@ def mx4_pack(codes, scales, K: int, stream=None) -> Mx4:
     """Lays row-major codes uint8 [rows][ceil(K / 2)] (the even element in the low nibble) and scale
     bytes uint8 [rows][ceil(K / 32)] out as an MX4 operand."""
     u8 = _torch().uint8
-    _require(codes.is_cuda and scales.device == codes.device and codes.dtype == u8 and scales.dtype == u8 and K >= 1 and
-             codes.dim() == 2 and tuple(scales.shape) == (codes.shape[0], -(-K // 32)) and
-             codes.shape[1] == -(-K // 2), "mx4_pack", "codes [rows][ceil(K / 2)] and scales [rows][ceil(K / 32)]")
+    if not (codes.is_cuda and scales.device == codes.device and codes.dtype == u8 and scales.dtype == u8 and K >= 1 and
+            codes.dim() == 2 and tuple(scales.shape) == (codes.shape[0], -(-K // 32)) and
+            codes.shape[1] == -(-K // 2)):
+        _refuse("mx4_pack", "codes [rows][ceil(K / 2)] and scales [rows][ceil(K / 32)]")
     rows = codes.shape[0]
-    out = _new_mx4(rows, K, codes.device, stream, "mx4_pack")
+    out = _new_mx4(rows, K, codes, stream, "mx4_pack")
     with _on_stream(stream):
         codes, scales = codes.contiguous(), scales.contiguous()
-    _call(apt_mx4_pack, codes.device, stream, (codes.data_ptr(), scales.data_ptr(), rows, K, out.data.data_ptr()))
+    _call("apt_mx4_pack", codes.device, stream, codes.data_ptr(), scales.data_ptr(), rows, K, out.data.data_ptr())
     return out
 
 
 def mx4_unpack(a: Mx4, stream=None):
     """(codes, scales) of an MX4 operand as mx4_pack takes them."""
-    torch = _torch()
-    with _on_stream(stream):
-        codes = torch.empty((a.rows, -(-a.K // 2)), dtype=torch.uint8, device=a.data.device)
-        scales = torch.empty((a.rows, -(-a.K // 32)), dtype=torch.uint8, device=a.data.device)
-    _call(apt_mx4_unpack, a.data.device, stream, (a.data.data_ptr(), a.rows, a.K, codes.data_ptr(), scales.data_ptr()))
+    codes = _new(a.data, (a.rows, -(-a.K // 2)), a.data.dtype, stream)
+    scales = _new(a.data, (a.rows, -(-a.K // 32)), a.data.dtype, stream)
+    _call("apt_mx4_unpack", a.data.device, stream, a.data.data_ptr(), a.rows, a.K, codes.data_ptr(), scales.data_ptr())
     return codes, scales
 
 
-def _product(M, w, dtype, need, device, stream, workspace, where):
-    """The output and the workspace (tensor or None, its bytes) of a product."""
-    torch = _torch()
-    _require(w.data.device == device, where, "the operands are on different devices")
-    with _on_stream(stream):
-        c = torch.empty((M, w.rows), dtype=dtype, device=device)
-        if workspace is None and need > 0:
-            workspace = torch.empty(need, dtype=torch.uint8, device=device)
-    if workspace is None:
-        return c, None, 0
-    _require(workspace.device == device and workspace.is_contiguous(), where, "a contiguous workspace on the device")
-    return c, workspace.data_ptr(), workspace.numel() * workspace.element_size()
-
-
-def mx4_gemm(a: Mx4, w: Mx4, dtype=None, stream=None, workspace=None):
-    """C = A W^T of two MX4 operands, [a.rows][w.rows] of `dtype` (fp16 by default).  A workspace of
-    apt_mx4_gemm_workspace_bytes is allocated with torch unless one is passed."""
+def mx4_gemm(a: Mx4, w: Mx4, dtype=None, stream=None):
+    """C = A W^T of two MX4 operands, [a.rows][w.rows] of `dtype` (fp16 by default)."""
     dtype = _torch().float16 if dtype is None else dtype
     t = _type(dtype, "mx4_gemm")
-    _require(a.K == w.K, "mx4_gemm", "operands of %d and %d values a row" % (a.K, w.K))
-    device = a.data.device
-    c, ws, n = _product(a.rows, w, dtype, apt_mx4_gemm_workspace_bytes(a.rows, w.rows, a.K), device, stream, workspace,
-                        "mx4_gemm")
-    _call(apt_mx4_gemm, device, stream,
-          (a.rows, w.rows, a.K, a.data.data_ptr(), w.data.data_ptr(), t, c.data_ptr(), ws, n))
+    ad, wd = a.data, w.data
+    device, M, N, K = ad.device, a.rows, w.rows, a.K
+    if K != w.K or wd.device != device:
+        _refuse("mx4_gemm", "operands of %d and %d values a row on %s and %s" % (K, w.K, device, wd.device))
+    c = _new(ad, (M, N), dtype, stream)
+    _call("apt_mx4_gemm", device, stream, M, N, K, ad.data_ptr(), wd.data_ptr(), t, c.data_ptr())
     return c
 
 
@@ -255,42 +265,52 @@ def mx4_gemm_act(x, w: Mx4, dtype=None, stream=None, workspace=None):
     M, K = x.shape
     dtype = x.dtype if dtype is None else dtype
     tx, t = _type(x.dtype, "mx4_gemm_act"), _type(dtype, "mx4_gemm_act")
-    _require(K == w.K, "mx4_gemm_act", "rows of %d values for weights of %d" % (K, w.K))
-    c, ws, n = _product(M, w, dtype, apt_mx4_gemm_act_workspace_bytes(M, w.rows, K), x.device, stream, workspace,
-                        "mx4_gemm_act")
-    _call(apt_mx4_gemm_act, x.device, stream,
-          (M, w.rows, K, x.data_ptr(), tx, stride, w.data.data_ptr(), t, c.data_ptr(), ws, n))
+    device, wd = x.device, w.data
+    if K != w.K or wd.device != device:
+        _refuse("mx4_gemm_act", "rows of %d values on %s for weights of %d on %s" % (K, device, w.K, wd.device))
+    N = w.rows
+    if workspace is None:
+        n = (_lib or lib()).apt_mx4_gemm_act_workspace_bytes(M, N, K)
+        if n:
+            workspace = _new(wd, n, wd.dtype, stream)
+    else:
+        if workspace.device != device or not workspace.is_contiguous():
+            _refuse("mx4_gemm_act", "a contiguous workspace on the rows' device is wanted")
+        n = workspace.numel() * workspace.element_size()
+    c = _new(x, (M, N), dtype, stream)
+    _call("apt_mx4_gemm_act", device, stream, M, N, K, x.data_ptr(), tx, stride, wd.data_ptr(), t, c.data_ptr(),
+          None if workspace is None else workspace.data_ptr(), n)
     return c
 
 
-def _norm_inputs(x, gain, residual, h, out_y, stream, where):
-    """Checked inputs of a norm: (x, the arguments up to `gain`, h, y).  h is given, allocated where
-    there is a residual, or None."""
+def _norm_inputs(x, gain, residual, h, stream, where):
+    """Checked inputs of a norm: x, the residual, the gain, h (given, or made where there is a residual,
+    or None) and the C arguments up to the gain."""
     torch = _torch()
-    _require(x.dtype in (torch.float16, torch.bfloat16), where, "fp16 or bf16 rows are wanted")
+    dtype = x.dtype
+    if dtype is not torch.float16 and dtype is not torch.bfloat16:
+        _refuse(where, "fp16 or bf16 rows are wanted")
     x, xs = _rows(x, where, stream)
     M, K = x.shape
-    r, rs = None, 0
+    rp, rs, gp = None, 0, None
     if residual is not None:
-        _require(residual.shape == x.shape and residual.dtype == x.dtype and residual.device == x.device, where,
-                 "a residual like x")
-        r, rs = _rows(residual, where, stream)
+        if residual.shape != x.shape or residual.dtype is not dtype or residual.device != x.device:
+            _refuse(where, "a residual like x is wanted")
+        residual, rs = _rows(residual, where, stream)
+        rp = residual.data_ptr()
     if gain is not None:
-        _require(tuple(gain.shape) == (K,) and gain.dtype == x.dtype and gain.device == x.device, where,
-                 "a gain of x's width, type and device")
-    with _on_stream(stream):
-        if gain is not None:
-            gain = gain.contiguous()
-        if h is not None:
-            _require(h.shape == x.shape and h.dtype == x.dtype and h.device == x.device and h.is_contiguous(), where,
-                     "a contiguous h like x")
-        elif residual is not None:
-            h = torch.empty((M, K), dtype=x.dtype, device=x.device)
-        y = torch.empty((M, K), dtype=x.dtype, device=x.device) if out_y else None
-    args = (M, K, _type(x.dtype, where), x.data_ptr(), xs, r.data_ptr() if r is not None else None, rs,
-            gain.data_ptr() if gain is not None else None)
-    # (copies made here stay alive until the call has been enqueued)
-    return (x, r, gain), args, h, y
+        if gain.dim() != 1 or gain.shape[0] != K or gain.dtype is not dtype or gain.device != x.device:
+            _refuse(where, "a gain of x's width, type and device is wanted")
+        if not gain.is_contiguous():
+            with _on_stream(stream):
+                gain = gain.contiguous()
+        gp = gain.data_ptr()
+    if h is not None:
+        if h.shape != x.shape or h.dtype is not dtype or h.device != x.device or not h.is_contiguous():
+            _refuse(where, "a contiguous h like x is wanted")
+    elif residual is not None:
+        h = _new_like(x, dtype, stream)
+    return x, residual, gain, h, (M, K, _type(dtype, where), x.data_ptr(), xs, rp, rs, gp)
 
 
 def rmsnorm_codes(x, gain, q: int, eps: float, residual=None, h=None, out_y: bool = False, stream=None):
@@ -299,27 +319,24 @@ def rmsnorm_codes(x, gain, q: int, eps: float, residual=None, h=None, out_y: boo
     h), and y behind them with out_y: h is x + residual, written to `h` where one is given (x or the
     residual themselves among them), to a new tensor where there is a residual, else None."""
     torch = _torch()
-    keep, args, h, y = _norm_inputs(x, gain, residual, h, out_y, stream, "rmsnorm_codes")
-    M, K = x.shape
-    with _on_stream(stream):
-        codes = torch.empty((M, K), dtype=torch.int8, device=x.device)
-        scale = torch.empty(M, dtype=torch.float16, device=x.device)
-    _call(apt_rmsnorm_codes, x.device, stream,
-          args + (eps, q, h.data_ptr() if h is not None else None, y.data_ptr() if y is not None else None,
-                  codes.data_ptr(), scale.data_ptr()))
-    del keep
+    # (copies that were made stay alive until the call has been enqueued)
+    x, residual, gain, h, args = _norm_inputs(x, gain, residual, h, stream, "rmsnorm_codes")
+    y = _new_like(x, x.dtype, stream) if out_y else None
+    codes = _new_like(x, torch.int8, stream)
+    scale = _new(x, x.shape[0], torch.float16, stream)
+    _call("apt_rmsnorm_codes", x.device, stream, *args, eps, q, None if h is None else h.data_ptr(),
+          None if y is None else y.data_ptr(), codes.data_ptr(), scale.data_ptr())
     return (codes, scale, h, y) if out_y else (codes, scale, h)
 
 
 def rmsnorm_mx4(x, gain, eps: float, residual=None, h=None, out_y: bool = False, stream=None):
     """As rmsnorm_codes with the row quantized to MX4.  Returns (Mx4, h), and y behind them with out_y."""
-    keep, args, h, y = _norm_inputs(x, gain, residual, h, out_y, stream, "rmsnorm_mx4")
-    M, K = x.shape
-    out = _new_mx4(M, K, x.device, stream, "rmsnorm_mx4")
-    _call(apt_rmsnorm_mx4, x.device, stream,
-          args + (eps, h.data_ptr() if h is not None else None, y.data_ptr() if y is not None else None,
-                  out.data.data_ptr()))
-    del keep
+    # (copies that were made stay alive until the call has been enqueued)
+    x, residual, gain, h, args = _norm_inputs(x, gain, residual, h, stream, "rmsnorm_mx4")
+    y = _new_like(x, x.dtype, stream) if out_y else None
+    out = _new_mx4(x.shape[0], x.shape[1], x, stream, "rmsnorm_mx4")
+    _call("apt_rmsnorm_mx4", x.device, stream, *args, eps, None if h is None else h.data_ptr(),
+          None if y is None else y.data_ptr(), out.data.data_ptr())
     return (out, h, y) if out_y else (out, h)
 
 
@@ -328,12 +345,13 @@ def dequantize(codes, scale, dtype=None, stream=None):
     torch = _torch()
     dtype = torch.float16 if dtype is None else dtype
     t = _type(dtype, "dequantize")
-    _require(codes.is_cuda and codes.dim() == 2 and codes.dtype == torch.int8 and scale.dtype == torch.float16 and
-             tuple(scale.shape) == (codes.shape[0],) and scale.device == codes.device, "dequantize",
-             "int8 codes [M][K] and fp16 scales [M]")
+    if not (codes.is_cuda and codes.dim() == 2 and codes.dtype is torch.int8 and scale.dtype is torch.float16 and
+            scale.dim() == 1 and scale.shape[0] == codes.shape[0] and scale.device == codes.device):
+        _refuse("dequantize", "int8 codes [M][K] and fp16 scales [M] are wanted")
+    if not (codes.is_contiguous() and scale.is_contiguous()):
+        with _on_stream(stream):
+            codes, scale = codes.contiguous(), scale.contiguous()
     M, K = codes.shape
-    with _on_stream(stream):
-        codes, scale = codes.contiguous(), scale.contiguous()
-        out = torch.empty((M, K), dtype=dtype, device=codes.device)
-    _call(apt_dequantize_codes, codes.device, stream, (codes.data_ptr(), scale.data_ptr(), M, K, t, out.data_ptr()))
+    out = _new_like(codes, dtype, stream)
+    _call("apt_dequantize_codes", codes.device, stream, codes.data_ptr(), scale.data_ptr(), M, K, t, out.data_ptr())
     return out

@@ -56,7 +56,8 @@ def test_pack_refuses(bad):
     assert apt.apt_mx4_unpack(a["mx"], a["rows"], a["K"], a["codes"], a["scales"], None) == BAD
 
 
-GEMM = dict(M=5, N=7, K=100, w_mx=P, type=BF16, c=P, workspace=P, workspace_bytes=1 << 30, stream=None)
+GEMM = dict(M=5, N=7, K=100, w_mx=P, type=BF16, c=P, stream=None)
+ACT = GEMM | dict(M=300, x=P, x_type=F16, x_stride=100, workspace=P, workspace_bytes=1 << 30)
 COMMON = [dict(M=0), dict(N=0), dict(K=0), dict(M=-1), dict(w_mx=None), dict(w_mx=P + 8), dict(type=0), dict(c=None),
           dict(c=P + 1), dict(type=F32, c=P + 2)]
 
@@ -69,21 +70,23 @@ def test_gemm_refuses(bad):
 @pytest.mark.parametrize("bad", COMMON + [dict(x=None), dict(x=P + 1), dict(x_type=9), dict(x_stride=99),
                                           dict(workspace=P + 1)])
 def test_gemm_act_refuses(bad):
-    assert apt.apt_mx4_gemm_act(**(GEMM | dict(x=P, x_type=F16, x_stride=100, M=300) | bad)) == BAD
+    assert apt.apt_mx4_gemm_act(**(ACT | bad)) == BAD
 
 
 def test_gemm_limits_and_workspace():
-    big = dict(GEMM, K=2 ** 24 + 1)
-    assert apt.apt_mx4_gemm(**(big | dict(a_mx=P))) == UNSUPPORTED
-    assert apt.apt_mx4_gemm_act(**(big | dict(x=P, x_type=F16, x_stride=2 ** 31))) == UNSUPPORTED
+    big = dict(K=2 ** 24 + 1)
+    assert apt.apt_mx4_gemm(**(GEMM | dict(a_mx=P) | big)) == UNSUPPORTED
+    assert apt.apt_mx4_gemm_act(**(ACT | big | dict(x_stride=2 ** 31))) == UNSUPPORTED
     assert apt.apt_mx4_gemm(**(GEMM | dict(a_mx=P, M=2 ** 31 - 1, N=2 ** 31 - 1))) == UNSUPPORTED
     for s in ((0, 1, 1), (1, 0, 1), (1, 1, 0), (1, 1, 2 ** 24 + 1)):
-        assert apt.apt_mx4_gemm_workspace_bytes(*s) == 0 and apt.apt_mx4_gemm_act_workspace_bytes(*s) == 0
+        assert apt.apt_mx4_gemm_act_workspace_bytes(*s) == 0
     need = apt.apt_mx4_gemm_act_workspace_bytes(300, 7, 100)
     assert need >= apt.apt_mx4_bytes(300, 100)
-    act = GEMM | dict(M=300, x=P, x_type=F16, x_stride=100)
-    assert apt.apt_mx4_gemm_act(**(act | dict(workspace=None))) == NO_SPACE
-    assert apt.apt_mx4_gemm_act(**(act | dict(workspace_bytes=need - 1))) == NO_SPACE
+    assert apt.apt_mx4_gemm_act(**(ACT | dict(workspace=None))) == NO_SPACE
+    assert apt.apt_mx4_gemm_act(**(ACT | dict(workspace_bytes=need - 1))) == NO_SPACE
+    # few rows are quantized by the product itself, unless they are too long for LDS
+    assert apt.apt_mx4_gemm_act_workspace_bytes(1, 7, 4096) == 0
+    assert apt.apt_mx4_gemm_act_workspace_bytes(1, 7, 2 ** 20) == apt.apt_mx4_bytes(1, 2 ** 20)
 
 
 NORM = dict(M=3, K=100, type=BF16, x=P, x_stride=100, residual=P, residual_stride=100, gain=P, eps=1e-5, h=2 * P,
