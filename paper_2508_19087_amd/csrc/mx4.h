@@ -49,12 +49,18 @@ struct Half {
   static constexpr uint32_t kInf = 0x7C00u;  // magnitude bits of infinity
   __device__ static float to_float(uint16_t v) { return (float)__builtin_bit_cast(_Float16, v); }
   __device__ static uint16_t from_float(float v) { return __builtin_bit_cast(uint16_t, (_Float16)v); }
+  __device__ static uint32_t pair(float a, float b) {  // rounded to nearest even, a in the low half
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{a, b}), f16x2));
+  }
 };
 struct Bf16 {
   static constexpr int kBytes = 2, kVec = 8;
   static constexpr uint32_t kInf = 0x7F80u;
   __device__ static float to_float(uint16_t v) { return __builtin_bit_cast(float, (uint32_t)v << 16); }
   __device__ static uint16_t from_float(float v) { return __builtin_bit_cast(uint16_t, (__bf16)v); }
+  __device__ static uint32_t pair(float a, float b) {
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{a, b}), bf16x2));
+  }
 };
 struct Float {
   static constexpr int kBytes = 4, kVec = 4;

@@ -66,6 +66,33 @@ __global__ __launch_bounds__(kWave* kWaves) void quantize_kernel(const uint8_t* 
   if (real && q < 2) *reinterpret_cast<uint32_t*>(o.scales + unit * kScaleBytes + q * 64 + s * 4) = bytes;
 }
 
+// The eight values of eight codes, in fp32 and in 16-bit types.
+__device__ __forceinline__ void values_of(uint32_t c, float scale, bool nan, float (&f)[8]) {
+  const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, scale, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, scale, 1);
+  const f32x2 d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, scale, 2), e = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, scale, 3);
+  const float v[8] = {a[0], a[1], b[0], b[1], d[0], d[1], e[0], e[1]};
+#pragma unroll
+  for (int j = 0; j < 8; ++j) f[j] = nan ? __builtin_nanf("") : v[j];
+}
+template <class T>
+__device__ __forceinline__ u32x4 packed_values(uint32_t c, float scale, bool nan) {
+  u32x4 v;
+  if constexpr (T::kInf == Half::kInf) {
+    v[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, scale, 0));
+    v[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, scale, 1));
+    v[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, scale, 2));
+    v[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, scale, 3));
+  } else {
+    v[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 0));
+    v[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 1));
+    v[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 2));
+    v[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 3));
+  }
+#pragma unroll
+  for (int j = 0; j < 4; ++j) v[j] = nan ? (T::kInf | 0x40u) * 0x00010001u : v[j];
+  return v;
+}
+
 // Values of an operand.  A wave takes 16 rows and one step again; its lane l
 // takes eight elements of a row at a time, rows l / 32 + 2 i, so that its
 // stores are whole 512-byte (16-bit types) or 1 KB runs of two rows.
@@ -89,19 +116,13 @@ __global__ __launch_bounds__(kWave* kWaves) void dequantize_kernel(Operand o, in
   for (int i = 0; i < 8; ++i) {
     const int64_t row = g * kGroup + lane / 32 + 2 * i;
     if (row >= rows) return;
-    float f[8];
     const float scale = scale_of(e[i]);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const uint32_t n = c[i] >> (4 * j) & 15u;
-      // the fp32 of magnitude n = (exponent, mantissa): 1.m 2^(ee - 1), m / 2 for ee = 0
-      const uint32_t mag = n & 7u;
-      const float a = mag < 2u ? 0.5f * (float)mag : __builtin_bit_cast(float, (mag << 22) + (126u << 23));
-      f[j] = e[i] == 255u ? __builtin_nanf("") : (n & 8u ? -a : a) * scale;
-    }
+    const bool nan = e[i] == 255u;
     const int64_t at = row * K + k;
     if constexpr (T::kBytes == 4) {
       float* const dst = reinterpret_cast<float*>(out) + at;
+      float f[8];
+      values_of(c[i], scale, nan, f);
       if (k + 8 <= K) {
         u32x4 lo, hi;
 #pragma unroll
@@ -118,18 +139,13 @@ __global__ __launch_bounds__(kWave* kWaves) void dequantize_kernel(Operand o, in
       }
     } else {
       uint16_t* const dst = reinterpret_cast<uint16_t*>(out) + at;
-      uint16_t h[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) h[j] = T::from_float(f[j]);
+      const u32x4 v = packed_values<T>(c[i], scale, nan);
       if (k + 8 <= K) {
-        u32x4 v;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] = (uint32_t)h[2 * j] | (uint32_t)h[2 * j + 1] << 16;
         *reinterpret_cast<any_u32x4*>(dst) = v;
       } else {
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-          if (k + j < K) dst[j] = h[j];
+          if (k + j < K) dst[j] = (uint16_t)(v[j / 2] >> (16 * (j % 2)));
       }
     }
   }

@@ -60,8 +60,7 @@ __device__ __forceinline__ void keep(const v16f& x) {
 // Four neighbouring outputs as bits of T: two dwords, or four of Float.
 template <class T>
 __device__ __forceinline__ u32x2 join4(float a, float b, float c, float d) {
-  return u32x2{(uint32_t)T::from_float(a) | (uint32_t)T::from_float(b) << 16,
-               (uint32_t)T::from_float(c) | (uint32_t)T::from_float(d) << 16};
+  return u32x2{T::pair(a, b), T::pair(c, d)};
 }
 
 // Stores one 16-byte piece of a row of the output from column n on.

@@ -13,13 +13,8 @@
 // move a code; squares of 11-bit values and their sums are exact to 2^-53 here,
 // so the order never shows in f, and y and its codes follow from f by single
 // IEEE operations.
-//
-// Codes: with h = y / (2 s), code = floor(h).  y and s have at most 11
-// significant bits, so an h that is no integer lies 2^-18 of itself or more
-// away from one, while fp32(y * fp32(0.5 / s)) is within 2^-23 of h: the bias
-// |h| 2^-20 lifts every integer over its own border and nothing else over the
-// next.
 #include "mx4.h"
+#include "rowcode.h"
 
 namespace apt {
 namespace {
@@ -36,7 +31,7 @@ struct NormArgs {
   const uint8_t* residual;
   int64_t r_stride;
   const uint8_t* gain;
-  double eps;
+  double inv_k, eps;  // 1 / K
   uint8_t* h;
   uint8_t* y;
   int q;
@@ -55,7 +50,7 @@ template <class T>
 __device__ __forceinline__ u32x4 join(const float (&f)[8]) {
   u32x4 v;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) v[i] = (uint32_t)T::from_float(f[2 * i]) | (uint32_t)T::from_float(f[2 * i + 1]) << 16;
+  for (int i = 0; i < 4; ++i) v[i] = T::pair(f[2 * i], f[2 * i + 1]);
   return v;
 }
 
@@ -70,50 +65,109 @@ __device__ __forceinline__ void store_vector(uint8_t* row, int k, int K, u32x4 v
   }
 }
 
-// Sum and largest value over the workgroup; `lds` holds a value per wave.
+// Sum and largest value over the workgroup; `lds` holds a value per wave.  Within
+// a wave four DPP steps give every 16-lane row its result and lane reads the
+// wave's (through LDS, six dependent swaps of a double take about 0.4 us more).
+template <int kCtrl>
+__device__ __forceinline__ double add_dpp(double v) {
+  const u32x2 b = __builtin_bit_cast(u32x2, v);
+  const u32x2 o = {(uint32_t)__builtin_amdgcn_update_dpp(0, (int)b[0], kCtrl, 0xF, 0xF, false),
+                   (uint32_t)__builtin_amdgcn_update_dpp(0, (int)b[1], kCtrl, 0xF, 0xF, false)};
+  return v + __builtin_bit_cast(double, o);
+}
+__device__ __forceinline__ double lane_of(double v, int lane) {
+  const u32x2 b = __builtin_bit_cast(u32x2, v);
+  const u32x2 o = {(uint32_t)__builtin_amdgcn_readlane((int)b[0], lane), (uint32_t)__builtin_amdgcn_readlane((int)b[1], lane)};
+  return __builtin_bit_cast(double, o);
+}
 __device__ __forceinline__ double block_sum(double v, double* lds) {
-  for (int off = 1; off < kWave; off <<= 1) v += __shfl_xor(v, off);
+  v = add_dpp<0xB1>(v);   // lane ^ 1
+  v = add_dpp<0x4E>(v);   // lane ^ 2
+  v = add_dpp<0x141>(v);  // the row's half mirrored
+  v = add_dpp<0x140>(v);  // the row mirrored
+  v = (lane_of(v, 0) + lane_of(v, 16)) + (lane_of(v, 32) + lane_of(v, 48));
+  const int waves = (int)blockDim.x / kWave;
+  if (waves == 1) return v;
   if (threadIdx.x % kWave == 0) lds[threadIdx.x / kWave] = v;
   __syncthreads();
   double sum = 0.0;
-  for (int w = 0; w < (int)blockDim.x / kWave; ++w) sum += lds[w];
+  for (int w = 0; w < waves; ++w) sum += lds[w];
   return sum;
 }
 __device__ __forceinline__ uint32_t block_max(uint32_t v, uint32_t* lds) {
-  for (int off = 1; off < kWave; off <<= 1) v = max(v, (uint32_t)__shfl_xor((int)v, off));
+  v = rowcode::wave_max(v);
+  const int waves = (int)blockDim.x / kWave;
+  if (waves == 1) return v;
   if (threadIdx.x % kWave == 0) lds[threadIdx.x / kWave] = v;
   __syncthreads();
   uint32_t m = 0u;
-  for (int w = 0; w < (int)blockDim.x / kWave; ++w) m = max(m, lds[w]);
+  for (int w = 0; w < waves; ++w) m = max(m, lds[w]);
   return m;
 }
 
-// A row's codes from its largest magnitude.
+// 1 / sqrt(v), to 2^-50 or better (v a normal number, 0 or infinite): the
+// hardware's estimate r, and with e = 1 - v r^2 the expansion of r (1 - e)^(-1/2)
+// to second order, twice (an estimate good to 2^-14 suffices).
+__device__ __forceinline__ double inverse_root(double v) {
+  double r = __builtin_amdgcn_rsq(v);
+  if (!(v > 0.0) || r == 0.0) return r;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const double e = __builtin_fma(-v * r, r, 1.0);
+    r = __builtin_fma(r * e, __builtin_fma(e, 0.375, 0.5), r);
+  }
+  return r;
+}
+
+// A row's codes from its largest magnitude: floor(h) of h = y / (2 s).  y and s
+// have at most 11 significant bits, so an h that is no integer lies 2^-18 of
+// itself or more away from one, while the product with the reciprocal is off by
+// 2^-22 at most: lifted by |h| 2^-20 it passes the border of an integer and no
+// other.  With a normal s, |h| is at most (2^q - 1) / 2 (1 + 2^-11) and its floor
+// in range; a subnormal s may be far from the quotient it rounds, and h further
+// out.
 struct CodeScale {
-  float rh;        // 0.5 / s
-  uint16_t bits;   // s
-  bool bad;
+  float rh;       // 0.5 / s
+  uint32_t bits;  // s
+  bool bad, clamp;
   template <class T>
   __device__ __forceinline__ void set(uint32_t m, int q) {
     const float top = (float)((1 << q) - 1);
-    const _Float16 s = (_Float16)__fdiv_rn(T::to_float((uint16_t)m), top);
-    bits = __builtin_bit_cast(uint16_t, s);
+    const _Float16 s16 = (_Float16)__fdiv_rn(T::to_float((uint16_t)m), top);
+    bits = __builtin_bit_cast(uint16_t, s16);
     bad = m >= T::kInf || bits >= 0x7C00u;
+    clamp = bits < 0x0400u;
+    rh = !bad && bits != 0u ? 0.5f * __builtin_amdgcn_rcpf((float)s16) : 0.0f;
     if (bad) bits = 0x7E00u;
-    rh = !bad && (float)s > 0.0f ? __fdiv_rn(0.5f, (float)s) : 0.0f;
   }
-  // code of y (0 in a bad row), as a byte
-  __device__ __forceinline__ uint32_t code(float y, int lo, int hi) const {
-    const float h = y * rh;
-    int c;
-    asm("v_cvt_flr_i32_f32 %0, %1" : "=v"(c) : "v"(__builtin_fmaf(__builtin_fabsf(h), 0x1p-20f, h)));
-    return (uint32_t)min(max(c, lo), hi) & 255u;
+  // codes of eight values, a byte each
+  __device__ __forceinline__ u32x2 codes(const float (&y)[8], int q) const {
+    if (bad) return u32x2{0u, 0u};
+    int v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float h = y[i] * rh;
+      asm("v_cvt_flr_i32_f32 %0, %1" : "=v"(v[i]) : "v"(__builtin_fmaf(__builtin_fabsf(h), 0x1p-20f, h)));
+    }
+    if (clamp) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = min(max(v[i], -(1 << (q - 1))), (1 << (q - 1)) - 1);
+    }
+    u32x2 c;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int* const b = v + 4 * i;
+      c[i] = __builtin_amdgcn_perm(__builtin_amdgcn_perm((uint32_t)b[3], (uint32_t)b[2], 0x0C0C0400u),
+                                   __builtin_amdgcn_perm((uint32_t)b[1], (uint32_t)b[0], 0x0C0C0400u), 0x05040100u);
+    }
+    return c;
   }
 };
 
 // T: element type; NV: vectors of 8 elements held per thread (0: none, the row
-// is read again in each pass); kCodes: q-bit codes, else MX4.
-template <class T, int NV, bool kCodes>
+// is read again in each pass); kCodes: q-bit codes, else MX4; kWhole: K is a
+// multiple of 8, so that no vector is cut by the row's end.
+template <class T, int NV, bool kCodes, bool kWhole>
 __global__ __launch_bounds__(kWave* kMaxWaves) void rmsnorm_kernel(NormArgs a) {
   __shared__ double lds_sum[kMaxWaves];
   __shared__ uint32_t lds_max[kMaxWaves];
@@ -131,6 +185,25 @@ __global__ __launch_bounds__(kWave* kMaxWaves) void rmsnorm_kernel(NormArgs a) {
   const int end = kCodes ? K : (K + kStep - 1) / kStep * kStep;
   const int vectors = (end + 7) / 8;
 
+  const u32x4 none = {0u, 0u, 0u, 0u};
+  auto load = [&](const uint8_t* p, int k) __attribute__((always_inline)) {
+    if constexpr (kWhole) return k < K ? load_whole<T>(p, k) : none;
+    else return load_vector<T>(p, k, K);
+  };
+  auto store = [&](uint8_t* p, int k, u32x4 v) __attribute__((always_inline)) {
+    if (kWhole && k < K) *reinterpret_cast<any_u32x4*>(p + (int64_t)k * 2) = v;
+    if (!kWhole) store_vector(p, k, K, v);
+  };
+  // (0 * an infinite or NaN factor: the elements behind K stay 0)
+  auto cut = [&](u32x4 v, int k) __attribute__((always_inline)) {
+    if (kWhole) return k < K ? v : none;
+    if (k + 8 > K) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (k + j >= K) v[j / 2] &= j % 2 ? 0x0000FFFFu : 0xFFFF0000u;
+    }
+    return v;
+  };
   auto sum_of = [&](u32x4 xv, u32x4 rv) __attribute__((always_inline)) {
     if (r == nullptr) return xv;
     float f[8], e[8];
@@ -159,21 +232,16 @@ __global__ __launch_bounds__(kWave* kMaxWaves) void rmsnorm_kernel(NormArgs a) {
     }
     return join<T>(v);
   };
-  auto factor = [&](double sum) __attribute__((always_inline)) { return (float)(1.0 / __builtin_sqrt(sum / (double)K + a.eps)); };
-  const int lo = -(1 << (a.q - 1)), hi = (1 << (a.q - 1)) - 1;
+  auto factor = [&](double sum) __attribute__((always_inline)) { return (float)inverse_root(__builtin_fma(sum, a.inv_k, a.eps)); };
   auto store_codes = [&](int k, u32x4 y, const CodeScale& cs) __attribute__((always_inline)) {
     float f[8];
     spread<T>(y, f);
-    u32x2 c = {0u, 0u};
-    if (!cs.bad) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) c[i / 4] |= cs.code(f[i], lo, hi) << (8 * (i % 4));
-    }
+    const u32x2 c = cs.codes(f, a.q);
     uint8_t* const dst = reinterpret_cast<uint8_t*>(a.codes) + row * K + k;
-    if (k + 8 <= K) {
+    if (kWhole ? k < K : k + 8 <= K) {
       typedef uint32_t any_u32x2 __attribute__((ext_vector_type(2), aligned(1)));
       *reinterpret_cast<any_u32x2*>(dst) = c;
-    } else {
+    } else if (!kWhole) {
 #pragma unroll
       for (int i = 0; i < 8; ++i)
         if (k + i < K) dst[i] = (uint8_t)(c[i / 4] >> (8 * (i % 4)));
@@ -193,7 +261,6 @@ __global__ __launch_bounds__(kWave* kMaxWaves) void rmsnorm_kernel(NormArgs a) {
     if (k % kBlock == 0) a.mx.scales[unit * kScaleBytes + b % 2 * 64 + s * 4 + b / 2] = (uint8_t)byte;
   };
 
-  const u32x4 none = {0u, 0u, 0u, 0u};
   if constexpr (NV > 0) {
     u32x4 v[NV], g[NV];
     {
@@ -201,9 +268,9 @@ __global__ __launch_bounds__(kWave* kMaxWaves) void rmsnorm_kernel(NormArgs a) {
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
         const int k = (i * (int)blockDim.x + tid) * 8;
-        v[i] = load_vector<T>(x, k, K);
-        rv[i] = r != nullptr ? load_vector<T>(r, k, K) : none;
-        g[i] = a.gain != nullptr ? load_vector<T>(a.gain, k, K) : none;
+        v[i] = load(x, k);
+        rv[i] = r != nullptr ? load(r, k) : none;
+        g[i] = a.gain != nullptr ? load(a.gain, k) : none;
       }
 #pragma unroll
       for (int i = 0; i < NV; ++i) v[i] = sum_of(v[i], rv[i]);
@@ -212,7 +279,7 @@ __global__ __launch_bounds__(kWave* kMaxWaves) void rmsnorm_kernel(NormArgs a) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int k = (i * (int)blockDim.x + tid) * 8;
-      if (hrow != nullptr) store_vector(hrow, k, K, v[i]);
+      if (hrow != nullptr) store(hrow, k, v[i]);
       sum += squares(v[i]);
     }
     const float f = factor(block_sum(sum, lds_sum));
@@ -220,13 +287,8 @@ __global__ __launch_bounds__(kWave* kMaxWaves) void rmsnorm_kernel(NormArgs a) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int k = (i * (int)blockDim.x + tid) * 8;
-      v[i] = normed(v[i], g[i], f);
-      if (k + 8 > K) {  // (0 * an infinite or NaN f: the elements behind K stay 0)
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (k + j >= K) v[i][j / 2] &= j % 2 ? 0x0000FFFFu : 0xFFFF0000u;
-      }
-      if (yrow != nullptr) store_vector(yrow, k, K, v[i]);
+      v[i] = cut(normed(v[i], g[i], f), k);
+      if (yrow != nullptr) store(yrow, k, v[i]);
       if (kCodes) m = fold_magnitude<T>(m, v[i]);
       else if (k < end) store_mx4(k, v[i]);
     }
@@ -235,34 +297,28 @@ __global__ __launch_bounds__(kWave* kMaxWaves) void rmsnorm_kernel(NormArgs a) {
       cs.set<T>(block_max(widest<T>(m), lds_max), a.q);
 #pragma unroll
       for (int i = 0; i < NV; ++i) store_codes((i * (int)blockDim.x + tid) * 8, v[i], cs);
-      if (tid == 0) a.scale[row] = cs.bits;
+      if (tid == 0) a.scale[row] = (uint16_t)cs.bits;
     }
   } else {
     auto load_h = [&](int k) __attribute__((always_inline)) {
-      return sum_of(load_vector<T>(x, k, K), r != nullptr ? load_vector<T>(r, k, K) : none);
+      return sum_of(load(x, k), r != nullptr ? load(r, k) : none);
     };
     double sum = 0.0;
     for (int i = tid; i < vectors; i += (int)blockDim.x) {
       const u32x4 h = load_h(i * 8);
-      if (hrow != nullptr) store_vector(hrow, i * 8, K, h);
+      if (hrow != nullptr) store(hrow, i * 8, h);
       sum += squares(h);
     }
     const float f = factor(block_sum(sum, lds_sum));
     // (h may have replaced x or the residual: it is read back, by the thread that wrote it)
     auto load_y = [&](int k) __attribute__((always_inline)) {
-      const u32x4 h = hrow != nullptr ? load_vector<T>(hrow, k, K) : load_h(k);
-      u32x4 y = normed(h, a.gain != nullptr ? load_vector<T>(a.gain, k, K) : none, f);
-      if (k + 8 > K) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (k + j >= K) y[j / 2] &= j % 2 ? 0x0000FFFFu : 0xFFFF0000u;
-      }
-      return y;
+      const u32x4 h = hrow != nullptr ? load(hrow, k) : load_h(k);
+      return cut(normed(h, a.gain != nullptr ? load(a.gain, k) : none, f), k);
     };
     uint32_t m = 0u;
     for (int i = tid; i < vectors; i += (int)blockDim.x) {
       const u32x4 y = load_y(i * 8);
-      if (yrow != nullptr) store_vector(yrow, i * 8, K, y);
+      if (yrow != nullptr) store(yrow, i * 8, y);
       if (kCodes) m = fold_magnitude<T>(m, y);
       else store_mx4(i * 8, y);
     }
@@ -270,7 +326,7 @@ __global__ __launch_bounds__(kWave* kMaxWaves) void rmsnorm_kernel(NormArgs a) {
       CodeScale cs;
       cs.set<T>(block_max(widest<T>(m), lds_max), a.q);
       for (int i = tid; i < vectors; i += (int)blockDim.x) store_codes(i * 8, load_y(i * 8), cs);
-      if (tid == 0) a.scale[row] = cs.bits;
+      if (tid == 0) a.scale[row] = (uint16_t)cs.bits;
     }
   }
 }
@@ -309,16 +365,24 @@ __global__ __launch_bounds__(256) void dequantize_codes_kernel(const int8_t* __r
   }
 }
 
-template <class T, bool kCodes>
-hipError_t launch_norm_of(const NormArgs& a, int64_t rows, hipStream_t s) {
+template <class T, bool kCodes, bool kWhole>
+hipError_t launch_norm_as(const NormArgs& a, int64_t rows, hipStream_t s) {
   // rows of the launch, by whole groups of 128 for the MX4 mapping
   const unsigned grid = (unsigned)(kCodes ? rows : (rows + 127) / 128 * 128);
   const int vectors = (kCodes ? a.K + 7 : (a.K + kStep - 1) / kStep * kStep) / 8;
   auto threads = [&](int per) { return dim3((unsigned)((vectors + per * kWave - 1) / (per * kWave) * kWave)); };
-  if (vectors <= 512) return launch_kernel(rmsnorm_kernel<T, 1, kCodes>, dim3(grid), threads(1), 0, s, a);
-  if (vectors <= 2048) return launch_kernel(rmsnorm_kernel<T, 2, kCodes>, dim3(grid), threads(2), 0, s, a);
-  if (vectors <= 4096) return launch_kernel(rmsnorm_kernel<T, 4, kCodes>, dim3(grid), threads(4), 0, s, a);
-  return launch_kernel(rmsnorm_kernel<T, 0, kCodes>, dim3(grid), dim3(kWave * kMaxWaves), 0, s, a);
+  // One vector per thread for few rows (a row alone, 1 x 4096: 3.3 us in a graph
+  // against 3.6 with two), two where rows queue and a wave's fixed share of the
+  // work counts (2048 x 4096 into codes: 14.1 against 14.6), or are long.
+  if (vectors <= 512 && rows < 1024) return launch_kernel(rmsnorm_kernel<T, 1, kCodes, kWhole>, dim3(grid), threads(1), 0, s, a);
+  if (vectors <= 2048) return launch_kernel(rmsnorm_kernel<T, 2, kCodes, kWhole>, dim3(grid), threads(2), 0, s, a);
+  if (vectors <= 4096) return launch_kernel(rmsnorm_kernel<T, 4, kCodes, kWhole>, dim3(grid), threads(4), 0, s, a);
+  return launch_kernel(rmsnorm_kernel<T, 0, kCodes, kWhole>, dim3(grid), dim3(kWave * kMaxWaves), 0, s, a);
+}
+
+template <class T, bool kCodes>
+hipError_t launch_norm_of(const NormArgs& a, int64_t rows, hipStream_t s) {
+  return a.K % 8 == 0 ? launch_norm_as<T, kCodes, true>(a, rows, s) : launch_norm_as<T, kCodes, false>(a, rows, s);
 }
 
 // A launch holds fewer than 2^32 threads: at 1024 a row, this many rows (whole
@@ -342,6 +406,7 @@ hipError_t launch_rmsnorm(int M, int K, int type, const void* x, int64_t x_strid
     if (residual != nullptr) a.residual = static_cast<const uint8_t*>(residual) + r0 * r_stride * 2;
     a.r_stride = r_stride;
     a.gain = static_cast<const uint8_t*>(gain);
+    a.inv_k = 1.0 / K;
     a.eps = eps;
     if (h != nullptr) a.h = static_cast<uint8_t*>(h) + r0 * K * 2;
     if (y != nullptr) a.y = static_cast<uint8_t*>(y) + r0 * K * 2;
