@@ -133,15 +133,38 @@ __device__ __forceinline__ uint32_t codes_of(const u32x4* v, float scale) {
   return c;
 }
 
-// One 16-byte vector of a row from element k on, at any byte; load_vector takes
-// elements from K on as zero bits.
+// One 16-byte vector of a row from element k on.  A vector load at an address
+// that is no multiple of 4 takes several times as long (16 rows of 2816 fp16
+// values into MX4: 4.6 us in a graph from odd elements, 3.0 from even ones), so
+// load_split reads the dwords that hold the vector and shifts them; it reads no
+// dword that holds none of it.
 template <class T>
 __device__ __forceinline__ u32x4 load_whole(const uint8_t* row, int k) {
   return *reinterpret_cast<const any_u32x4*>(row + (int64_t)k * T::kBytes);
 }
+typedef uint32_t dword_u32x4 __attribute__((ext_vector_type(4), aligned(4)));
 template <class T>
-__device__ __forceinline__ u32x4 load_vector(const uint8_t* row, int k, int K) {
-  if (k + T::kVec <= K) return load_whole<T>(row, k);
+__device__ __forceinline__ u32x4 load_split(const uint8_t* row, int k) {
+  if constexpr (T::kBytes == 4) return load_whole<T>(row, k);
+  const uint8_t* const p = row + (int64_t)k * T::kBytes;
+  const uint32_t odd = (uint32_t)reinterpret_cast<uintptr_t>(p) & 2u;
+  const u32x4 v = *reinterpret_cast<const dword_u32x4*>(p - odd);
+  const uint32_t last = *reinterpret_cast<const uint32_t*>(p - odd + (odd ? 16 : 12));
+  const uint32_t s = odd * 8u;
+  return u32x4{__builtin_amdgcn_alignbit(v[1], v[0], s), __builtin_amdgcn_alignbit(v[2], v[1], s),
+               __builtin_amdgcn_alignbit(v[3], v[2], s), __builtin_amdgcn_alignbit(last, v[3], s)};
+}
+// The same near a row's end, in two steps so that several loads leave before the
+// first is waited for: load_near reads the vector, or the row's last whole one
+// where it would cross the end, and settle shifts that one down and leaves zero
+// bits from element K on.  (kSplit: rows may start at any element.  Rows shorter
+// than a vector take element loads.)
+template <class T, bool kSplit>
+__device__ __forceinline__ u32x4 load_near(const uint8_t* row, int k, int K) {
+  if (K >= T::kVec) {
+    const int at = min(k, K - T::kVec);
+    return kSplit ? load_split<T>(row, at) : load_whole<T>(row, at);
+  }
   u32x4 v = {0u, 0u, 0u, 0u};
   if constexpr (T::kBytes == 4) {
     const uint32_t* const p = reinterpret_cast<const uint32_t*>(row);
@@ -155,6 +178,55 @@ __device__ __forceinline__ u32x4 load_vector(const uint8_t* row, int k, int K) {
       if (k + i < K) v[i / 2] |= (uint32_t)p[k + i] << (16 * (i % 2));
   }
   return v;
+}
+template <class T>
+__device__ __forceinline__ u32x4 settle(u32x4 v, int k, int K) {
+  const int over = k + T::kVec - K;  // elements past the end
+  if (K < T::kVec || __builtin_amdgcn_ballot_w64(over > 0) == 0ull) return v;
+  const uint32_t bits = (uint32_t)max(over, 0) * (8 * T::kBytes);
+  // down by two dwords, one, and what is left of one (0 or 16 bits)
+  u32x4 r = v;
+  r = bits & 64u ? u32x4{r[2], r[3], 0u, 0u} : r;
+  r = bits & 32u ? u32x4{r[1], r[2], r[3], 0u} : r;
+  if constexpr (T::kBytes == 2)
+    r = u32x4{__builtin_amdgcn_alignbit(r[1], r[0], bits), __builtin_amdgcn_alignbit(r[2], r[1], bits),
+              __builtin_amdgcn_alignbit(r[3], r[2], bits), __builtin_amdgcn_alignbit(0u, r[3], bits)};
+  return bits >= 128u ? u32x4{0u, 0u, 0u, 0u} : r;
+}
+
+// The first n (at most 16) bytes of a vector to any byte address, n a multiple of
+// kBytes: whole, or as pieces of 8, 4, 2 and 1 bytes.
+template <int kBytes>
+__device__ __forceinline__ void store_bytes(uint8_t* dst, int n, u32x4 v) {
+  typedef uint32_t any_u32x2 __attribute__((ext_vector_type(2), aligned(1)));
+  typedef uint32_t any_u32 __attribute__((aligned(1)));
+  typedef uint16_t any_u16 __attribute__((aligned(1)));
+  if (n >= 16) {
+    *reinterpret_cast<any_u32x4*>(dst) = v;
+    return;
+  }
+  uint64_t left = (uint64_t)v[0] | (uint64_t)v[1] << 32;
+  if (n & 8) {
+    *reinterpret_cast<any_u32x2*>(dst) = u32x2{v[0], v[1]};
+    dst += 8;
+    left = (uint64_t)v[2] | (uint64_t)v[3] << 32;
+  }
+  if (n & 4) {
+    *reinterpret_cast<any_u32*>(dst) = (uint32_t)left;
+    dst += 4;
+    left >>= 32;
+  }
+  if (kBytes <= 2 && (n & 2)) {
+    *reinterpret_cast<any_u16*>(dst) = (uint16_t)left;
+    dst += 2;
+    left >>= 16;
+  }
+  if (kBytes == 1 && (n & 1)) *dst = (uint8_t)left;
+}
+// A vector of a row from element k on, as far as the row goes.
+template <class T>
+__device__ __forceinline__ void store_vector(uint8_t* row, int k, int K, u32x4 v) {
+  if (k < K) store_bytes<T::kBytes>(row + (int64_t)k * T::kBytes, (K - k < T::kVec ? K - k : T::kVec) * T::kBytes, v);
 }
 
 // Launches (arguments validated by the ABI).

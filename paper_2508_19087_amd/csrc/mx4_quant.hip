@@ -36,16 +36,29 @@ __global__ __launch_bounds__(kWave* kWaves) void quantize_kernel(const uint8_t* 
   const uint8_t* const src = x + (real ? row : 0) * stride * T::kBytes;
   u32x4 v[2][kPieces];
   // (rows past the edge read the first row and store nothing)
-  if (k0 + kStep <= K) {
+  const bool dwords = T::kBytes == 4 || ((reinterpret_cast<uintptr_t>(x) | (uintptr_t)(stride * 2)) & 3) == 0;
+  auto place = [&](int u, int i) __attribute__((always_inline)) { return k0 + (q + 4 * u) * kBlock + i * T::kVec; };
+  if (k0 + kStep <= K && dwords) {
 #pragma unroll
     for (int u = 0; u < 2; ++u)
 #pragma unroll
-      for (int i = 0; i < kPieces; ++i) v[u][i] = load_whole<T>(src, k0 + (q + 4 * u) * kBlock + i * T::kVec);
+      for (int i = 0; i < kPieces; ++i) v[u][i] = load_whole<T>(src, place(u, i));
   } else {
+    if (dwords) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) v[u][i] = load_near<T, false>(src, place(u, i), K);
+    } else {
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) v[u][i] = load_near<T, true>(src, place(u, i), K);
+    }
 #pragma unroll
     for (int u = 0; u < 2; ++u)
 #pragma unroll
-      for (int i = 0; i < kPieces; ++i) v[u][i] = load_vector<T>(src, k0 + (q + 4 * u) * kBlock + i * T::kVec, K);
+      for (int i = 0; i < kPieces; ++i) v[u][i] = settle<T>(v[u][i], place(u, i), K);
   }
   uint32_t bytes = 0u;
 #pragma unroll
@@ -118,35 +131,20 @@ __global__ __launch_bounds__(kWave* kWaves) void dequantize_kernel(Operand o, in
     if (row >= rows) return;
     const float scale = scale_of(e[i]);
     const bool nan = e[i] == 255u;
-    const int64_t at = row * K + k;
+    uint8_t* const dst = out + row * K * T::kBytes;
     if constexpr (T::kBytes == 4) {
-      float* const dst = reinterpret_cast<float*>(out) + at;
       float f[8];
       values_of(c[i], scale, nan, f);
-      if (k + 8 <= K) {
-        u32x4 lo, hi;
+      u32x4 lo, hi;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          lo[j] = __builtin_bit_cast(uint32_t, f[j]);
-          hi[j] = __builtin_bit_cast(uint32_t, f[4 + j]);
-        }
-        reinterpret_cast<any_u32x4*>(dst)[0] = lo;
-        reinterpret_cast<any_u32x4*>(dst)[1] = hi;
-      } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (k + j < K) dst[j] = f[j];
+      for (int j = 0; j < 4; ++j) {
+        lo[j] = __builtin_bit_cast(uint32_t, f[j]);
+        hi[j] = __builtin_bit_cast(uint32_t, f[4 + j]);
       }
+      store_vector<T>(dst, k, K, lo);
+      store_vector<T>(dst, k + 4, K, hi);
     } else {
-      uint16_t* const dst = reinterpret_cast<uint16_t*>(out) + at;
-      const u32x4 v = packed_values<T>(c[i], scale, nan);
-      if (k + 8 <= K) {
-        *reinterpret_cast<any_u32x4*>(dst) = v;
-      } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (k + j < K) dst[j] = (uint16_t)(v[j / 2] >> (16 * (j % 2)));
-      }
+      store_vector<T>(dst, k, K, packed_values<T>(c[i], scale, nan));
     }
   }
 }

@@ -72,15 +72,18 @@ struct RowShare {
       const int m = x / per_row, k = (x - m * per_row) * 8;
       const uint8_t* const row = p.x + m * p.x_stride * X::kBytes;
 #pragma unroll
-      for (int j = 0; j < kPieces; ++j) v[i][j] = load_vector<X>(row, k + j * X::kVec, p.K);
+      for (int j = 0; j < kPieces; ++j) v[i][j] = load_near<X, true>(row, k + j * X::kVec, p.K);
     }
   }
-  __device__ __forceinline__ void store(const ThinParams& p, uint8_t* lds, int i0) const {
+  __device__ __forceinline__ void store(const ThinParams& p, uint8_t* lds, int i0) {
     const int per_row = p.steps * (kStep / 8), all = per_row * p.M;
     uint8_t* const scales = lds + p.steps * p.M * (kStep / 2);
 #pragma unroll
     for (int i = 0; i < kHeld; ++i) {
       const int x = i0 + i * kThinWaves * kWave;
+      const int row = min(x, all - 1) / per_row, y = min(x, all - 1) - row * per_row;  // eighth y of the row
+#pragma unroll
+      for (int j = 0; j < kPieces; ++j) v[i][j] = settle<X>(v[i][j], y * 8 + j * X::kVec, p.K);
       uint32_t m = 0u;
 #pragma unroll
       for (int j = 0; j < kPieces; ++j) m = fold_magnitude<X>(m, v[i][j]);
@@ -90,7 +93,6 @@ struct RowShare {
       const uint32_t byte = scale_byte<X>(m);
       const uint32_t c = byte == 255u ? 0u : codes_of<X>(v[i], scale_of(byte));
       if (x >= all) continue;
-      const int row = x / per_row, y = x - row * per_row;  // eighth y of the row
       const int block = y / 4;
       *reinterpret_cast<uint32_t*>(lds + (block * p.M + row) * 16 + y % 4 * 4) = c;
       if (y % 4 == 0) scales[((block / 8 * 2 + block % 2) * p.M + row) * 4 + block % 8 / 2] = (uint8_t)byte;

@@ -63,22 +63,6 @@ __device__ __forceinline__ u32x2 join4(float a, float b, float c, float d) {
   return u32x2{T::pair(a, b), T::pair(c, d)};
 }
 
-// Stores one 16-byte piece of a row of the output from column n on.
-template <class T>
-__device__ __forceinline__ void store_piece(uint8_t* row, int n, int N, u32x4 v) {
-  if (n + T::kVec <= N) {
-    *reinterpret_cast<any_u32x4*>(row + (int64_t)n * T::kBytes) = v;
-  } else if constexpr (T::kBytes == 4) {
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (n + j < N) reinterpret_cast<uint32_t*>(row)[n + j] = v[j];
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (n + j < N) reinterpret_cast<uint16_t*>(row)[n + j] = (uint16_t)(v[j / 2] >> (16 * (j % 2)));
-  }
-}
-
 // WD: steps whose weights a wave holds, 2 or 4 (the loads run WD - 1 steps ahead).
 template <class T, int MB, int NB, int WD>
 __global__ __launch_bounds__(kTileWaves* kWave, (MB * NB >= 12 ? 1 : 2)) void tile_kernel(GemmParams p) {
@@ -295,7 +279,7 @@ __global__ __launch_bounds__(kTileWaves* kWave, (MB * NB >= 12 ? 1 : 2)) void ti
         const u32x4 v = *reinterpret_cast<const u32x4*>(slot + row * kStride + piece * 16);
         const int64_t m = (int64_t)m0 * (MB * 32) + a * 32 + row;
         const int n = nw + b0 * 32 + piece * T::kVec;
-        if (m < p.M && n < p.N) store_piece<T>(p.c + m * p.N * T::kBytes, n, p.N, v);
+        if (m < p.M) store_vector<T>(p.c + m * p.N * T::kBytes, n, p.N, v);
       }
       __builtin_amdgcn_s_waitcnt(0xc07f);  // reads done before the slot is rewritten
       __builtin_amdgcn_wave_barrier();

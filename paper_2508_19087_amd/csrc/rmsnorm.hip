@@ -54,17 +54,6 @@ __device__ __forceinline__ u32x4 join(const float (&f)[8]) {
   return v;
 }
 
-__device__ __forceinline__ void store_vector(uint8_t* row, int k, int K, u32x4 v) {
-  if (k + 8 <= K) {
-    *reinterpret_cast<any_u32x4*>(row + (int64_t)k * 2) = v;
-  } else {
-    uint16_t* const p = reinterpret_cast<uint16_t*>(row);
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (k + i < K) p[k + i] = (uint16_t)(v[i / 2] >> (16 * (i % 2)));
-  }
-}
-
 // Sum and largest value over the workgroup; `lds` holds a value per wave.  Within
 // a wave four DPP steps give every 16-lane row its result and lane reads the
 // wave's (through LDS, six dependent swaps of a double take about 0.4 us more).
@@ -166,7 +155,8 @@ struct CodeScale {
 
 // T: element type; NV: vectors of 8 elements held per thread (0: none, the row
 // is read again in each pass); kCodes: q-bit codes, else MX4; kWhole: K is a
-// multiple of 8, so that no vector is cut by the row's end.
+// multiple of 8, so that no vector is cut by the row's end, and every row that is
+// read starts at a multiple of 4 bytes.
 template <class T, int NV, bool kCodes, bool kWhole>
 __global__ __launch_bounds__(kWave* kMaxWaves) void rmsnorm_kernel(NormArgs a) {
   __shared__ double lds_sum[kMaxWaves];
@@ -188,11 +178,12 @@ __global__ __launch_bounds__(kWave* kMaxWaves) void rmsnorm_kernel(NormArgs a) {
   const u32x4 none = {0u, 0u, 0u, 0u};
   auto load = [&](const uint8_t* p, int k) __attribute__((always_inline)) {
     if constexpr (kWhole) return k < K ? load_whole<T>(p, k) : none;
-    else return load_vector<T>(p, k, K);
+    else return load_near<T, true>(p, k, K);
   };
+  auto settled = [&](u32x4 v, int k) __attribute__((always_inline)) { return kWhole ? v : settle<T>(v, k, K); };
   auto store = [&](uint8_t* p, int k, u32x4 v) __attribute__((always_inline)) {
     if (kWhole && k < K) *reinterpret_cast<any_u32x4*>(p + (int64_t)k * 2) = v;
-    if (!kWhole) store_vector(p, k, K, v);
+    if (!kWhole) store_vector<T>(p, k, K, v);
   };
   // (0 * an infinite or NaN factor: the elements behind K stay 0)
   auto cut = [&](u32x4 v, int k) __attribute__((always_inline)) {
@@ -237,14 +228,9 @@ __global__ __launch_bounds__(kWave* kMaxWaves) void rmsnorm_kernel(NormArgs a) {
     float f[8];
     spread<T>(y, f);
     const u32x2 c = cs.codes(f, a.q);
-    uint8_t* const dst = reinterpret_cast<uint8_t*>(a.codes) + row * K + k;
-    if (kWhole ? k < K : k + 8 <= K) {
-      typedef uint32_t any_u32x2 __attribute__((ext_vector_type(2), aligned(1)));
-      *reinterpret_cast<any_u32x2*>(dst) = c;
-    } else if (!kWhole) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (k + i < K) dst[i] = (uint8_t)(c[i / 4] >> (8 * (i % 4)));
+    if (k < K) {
+      uint8_t* const dst = reinterpret_cast<uint8_t*>(a.codes) + row * K + k;
+      store_bytes<1>(dst, kWhole ? 8 : min(K - k, 8), u32x4{c[0], c[1], 0u, 0u});
     }
   };
   // (the four lanes of a block are neighbours, active together)
@@ -273,7 +259,11 @@ __global__ __launch_bounds__(kWave* kMaxWaves) void rmsnorm_kernel(NormArgs a) {
         g[i] = a.gain != nullptr ? load(a.gain, k) : none;
       }
 #pragma unroll
-      for (int i = 0; i < NV; ++i) v[i] = sum_of(v[i], rv[i]);
+      for (int i = 0; i < NV; ++i) {
+        const int k = (i * (int)blockDim.x + tid) * 8;
+        v[i] = sum_of(settled(v[i], k), settled(rv[i], k));
+        g[i] = settled(g[i], k);
+      }
     }
     double sum = 0.0;
 #pragma unroll
@@ -301,7 +291,8 @@ __global__ __launch_bounds__(kWave* kMaxWaves) void rmsnorm_kernel(NormArgs a) {
     }
   } else {
     auto load_h = [&](int k) __attribute__((always_inline)) {
-      return sum_of(load(x, k), r != nullptr ? load(r, k) : none);
+      const u32x4 xv = load(x, k), rv = r != nullptr ? load(r, k) : none;
+      return sum_of(settled(xv, k), settled(rv, k));
     };
     double sum = 0.0;
     for (int i = tid; i < vectors; i += (int)blockDim.x) {
@@ -312,8 +303,9 @@ __global__ __launch_bounds__(kWave* kMaxWaves) void rmsnorm_kernel(NormArgs a) {
     const float f = factor(block_sum(sum, lds_sum));
     // (h may have replaced x or the residual: it is read back, by the thread that wrote it)
     auto load_y = [&](int k) __attribute__((always_inline)) {
-      const u32x4 h = hrow != nullptr ? load(hrow, k) : load_h(k);
-      return cut(normed(h, a.gain != nullptr ? load(a.gain, k) : none, f), k);
+      const u32x4 g = a.gain != nullptr ? load(a.gain, k) : none;
+      const u32x4 h = hrow != nullptr ? settled(load(hrow, k), k) : load_h(k);
+      return cut(normed(h, settled(g, k), f), k);
     };
     uint32_t m = 0u;
     for (int i = tid; i < vectors; i += (int)blockDim.x) {
@@ -342,10 +334,9 @@ __global__ __launch_bounds__(256) void dequantize_codes_kernel(const int8_t* __r
   if (k >= K) return;
   const float s = Half::to_float(scale[row]);
   const int8_t* const src = codes + row * K + k;
-  const bool whole = k + 8 <= K;
   typedef uint32_t any_u32x2 __attribute__((ext_vector_type(2), aligned(1)));
   u32x2 c = {0u, 0u};
-  if (whole) {
+  if (k + 8 <= K) {
     c = *reinterpret_cast<const any_u32x2*>(src);
   } else {
 #pragma unroll
@@ -355,13 +346,18 @@ __global__ __launch_bounds__(256) void dequantize_codes_kernel(const int8_t* __r
   float f[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) f[i] = (float)(2 * (int)(int8_t)(c[i / 4] >> (8 * (i % 4))) + 1) * s;
+  uint8_t* const dst = out + row * K * T::kBytes;
   if constexpr (T::kBytes == 4) {
-    float* const dst = reinterpret_cast<float*>(out) + row * K + k;
+    u32x4 lo, hi;
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (whole || k + i < K) dst[i] = f[i];
+    for (int i = 0; i < 4; ++i) {
+      lo[i] = __builtin_bit_cast(uint32_t, f[i]);
+      hi[i] = __builtin_bit_cast(uint32_t, f[4 + i]);
+    }
+    store_vector<T>(dst, k, K, lo);
+    store_vector<T>(dst, k + 4, K, hi);
   } else {
-    store_vector(out + row * K * 2, k, K, join<T>(f));
+    store_vector<T>(dst, k, K, join<T>(f));
   }
 }
 
@@ -382,7 +378,10 @@ hipError_t launch_norm_as(const NormArgs& a, int64_t rows, hipStream_t s) {
 
 template <class T, bool kCodes>
 hipError_t launch_norm_of(const NormArgs& a, int64_t rows, hipStream_t s) {
-  return a.K % 8 == 0 ? launch_norm_as<T, kCodes, true>(a, rows, s) : launch_norm_as<T, kCodes, false>(a, rows, s);
+  uintptr_t at = reinterpret_cast<uintptr_t>(a.x) | reinterpret_cast<uintptr_t>(a.gain) | (uintptr_t)(a.x_stride * 2);
+  if (a.residual != nullptr) at |= reinterpret_cast<uintptr_t>(a.residual) | (uintptr_t)(a.r_stride * 2);
+  return a.K % 8 == 0 && at % 4 == 0 ? launch_norm_as<T, kCodes, true>(a, rows, s)
+                                     : launch_norm_as<T, kCodes, false>(a, rows, s);
 }
 
 // A launch holds fewer than 2^32 threads: at 1024 a row, this many rows (whole
