@@ -2,6 +2,7 @@
 // gfx950: the choice among the kernels of mx4_thin.h and mx4_tile.h, and their
 // launches.
 #include <algorithm>
+#include <cmath>
 
 #include "mx4_thin.h"
 
@@ -11,19 +12,21 @@ namespace {
 using namespace mx4;
 
 // A tile shape and what a step of 256 elements of K costs a workgroup of it, in
-// us: on its own on a compute unit, and its share of a compute unit's
-// throughput when the whole chip is busy.  Measured at bf16 output from the
-// slopes over K = 2048..8192 of 64, 256 and 2048 rows by 4096 and 11008 columns.
+// us: with few compute units busy, with each running one (in between in
+// proportion: what they share, clock, caches and memory, counts long before the
+// chip is full), and its share where each runs several.  `fixed`: what it needs
+// besides more than the others.  Measured at bf16 output on 64 to 2048 rows by
+// 4096 and 11008 columns, K = 4096 to 11008.
 struct Tile {
   int mb, nb;
-  double alone, share, fixed;
+  double few, one, share, fixed;
 };
 constexpr Tile kTiles[] = {
-    {1, 1, 0.28, 0.28, 0.0},  // 32 x 128
-    {2, 1, 0.33, 0.36, 0.0},  // 64 x 128
-    {4, 1, 0.39, 0.58, 0.0},  // 128 x 128
-    {4, 2, 0.52, 0.84, 0.0},  // 128 x 256
-    {8, 2, 0.94, 1.54, 4.0},  // 256 x 256, one workgroup per compute unit: its epilogue stands alone
+    {1, 1, 0.22, 0.25, 0.25, 0.0},  // 32 x 128
+    {2, 1, 0.25, 0.34, 0.31, 0.0},  // 64 x 128
+    {4, 1, 0.36, 0.50, 0.55, 0.0},  // 128 x 128
+    {4, 2, 0.32, 1.00, 0.84, 0.0},  // 128 x 256
+    {8, 2, 0.85, 1.60, 1.60, 4.0},  // 256 x 256, one workgroup per compute unit: its epilogue stands alone
 };
 constexpr int kNumTiles = sizeof(kTiles) / sizeof(kTiles[0]);
 constexpr double kUnits = 256.0;  // compute units
@@ -40,9 +43,9 @@ int64_t tiles_of(int M, int N, const Tile& t) {
   return ((int64_t)M + t.mb * 32 - 1) / (t.mb * 32) * (((int64_t)N + t.nb * 128 - 1) / (t.nb * 128));
 }
 
-double per_step(double tiles, double alone, double share) {
+double per_step(double tiles, const Tile& t) {
   const double load = tiles / kUnits;
-  return std::max(alone, share * (load > 1.0 ? (double)(int64_t)(load + 0.999) : load));
+  return load <= 1.0 ? t.few + (t.one - t.few) * load : t.share * std::ceil(load);
 }
 
 // The kernel of a problem: -1 for the few-row kernel, else an index into kTiles.
@@ -51,17 +54,17 @@ double per_step(double tiles, double alone, double share) {
 // apply; between them the modelled times decide (64 x 11008 x 4096 9.9 against
 // 7.7 us on 32 x 128 tiles, 64 x 4096 x 11008 9.2 against 12.8).  Among the tiles
 // a large one costs fewer loads per MFMA and a small one fills the chip:
-// 2048 x 11008 x 4096 takes 49 us at 128 x 256 and 56, 68, 92 at 128, 64 and 32 x
-// 128; 333 x 5003 x 2999 7.6 us at 64 x 128, 9.1 and 12.7 at 128 x 128 and 128 x
-// 256.  What all of them need besides (launch, first loads, output) is left out.
+// 2048 x 11008 x 4096 takes 46 us at 128 x 256 and 59, 56, 64, 90 at 256 x 256,
+// 128, 64 and 32 x 128; 333 x 5003 x 2999 7.7 us at 64 x 128, 9.1 and 11.9 at 128 x
+// 128 and 128 x 256; 1024 x 4096 x 11008 27 at 128 x 128 and 31 at 128 x 256.
 int kernel_of(int M, int N, int K) {
   if (M <= 32) return -1;
   const double S = steps(K);
   int best = -1;
-  double least = M <= kThinRows ? S * std::max(0.17, 0.12 * (double)groups(N) / kUnits) - 1.5 : 1e30;
+  double least = M <= kThinRows ? S * std::max(0.17, 0.12 * (double)groups(N) / kUnits) - 0.5 : 1e30;
   for (int i = 0; i < kNumTiles; ++i) {
     const Tile& t = kTiles[i];
-    const double us = S * per_step((double)tiles_of(M, N, t), t.alone, t.share) + t.fixed;
+    const double us = S * per_step((double)tiles_of(M, N, t), t) + t.fixed;
     if (us < least) {
       least = us;
       best = i;

@@ -79,18 +79,17 @@ __global__ __launch_bounds__(kWave* kWaves) void quantize_kernel(const uint8_t* 
   if (real && q < 2) *reinterpret_cast<uint32_t*>(o.scales + unit * kScaleBytes + q * 64 + s * 4) = bytes;
 }
 
-// The eight values of eight codes, in fp32 and in 16-bit types.
-__device__ __forceinline__ void values_of(uint32_t c, float scale, bool nan, float (&f)[8]) {
-  const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, scale, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, scale, 1);
-  const f32x2 d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, scale, 2), e = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, scale, 3);
-  const float v[8] = {a[0], a[1], b[0], b[1], d[0], d[1], e[0], e[1]};
-#pragma unroll
-  for (int j = 0; j < 8; ++j) f[j] = nan ? __builtin_nanf("") : v[j];
-}
+// A vector of values: of eight codes in 16-bit types, of four in fp32.
 template <class T>
 __device__ __forceinline__ u32x4 packed_values(uint32_t c, float scale, bool nan) {
   u32x4 v;
-  if constexpr (T::kInf == Half::kInf) {
+  if constexpr (T::kBytes == 4) {
+    const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, scale, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, scale, 1);
+    const float f[4] = {a[0], a[1], b[0], b[1]};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = nan ? 0x7FC00000u : __builtin_bit_cast(uint32_t, f[j]);
+    return v;
+  } else if constexpr (T::kInf == Half::kInf) {
     v[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, scale, 0));
     v[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, scale, 1));
     v[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, scale, 2));
@@ -106,46 +105,34 @@ __device__ __forceinline__ u32x4 packed_values(uint32_t c, float scale, bool nan
   return v;
 }
 
-// Values of an operand.  A wave takes 16 rows and one step again; its lane l
-// takes eight elements of a row at a time, rows l / 32 + 2 i, so that its
-// stores are whole 512-byte (16-bit types) or 1 KB runs of two rows.
-template <class T>
+// Values of an operand.  A wave takes 16 rows and one step again; its lanes take
+// the elements of a row in order, eight at a time for 16-bit types (rows l / 32 +
+// 2 i) and four for fp32, so that every store instruction writes whole 512-byte
+// or 1 KB runs.
+template <class T, bool kStream>
 __global__ __launch_bounds__(kWave* kWaves) void dequantize_kernel(Operand o, int rows, int K, uint8_t* __restrict__ out) {
+  constexpr int kElems = T::kVec;                  // per lane and row
+  constexpr int kAtOnce = kWave * kElems / kStep;  // rows per store
+  constexpr int kTurns = kGroup / kAtOnce;
   const int lane = threadIdx.x % kWave;
   const int64_t unit = (int64_t)blockIdx.x * kWaves + threadIdx.x / kWave;
   if (unit >= o.groups * o.steps) return;
   const int64_t g = unit / o.steps;
-  const int p = lane % 32, b = p / 4;  // eighth of the step, its block
-  const int k = (int)(unit % o.steps) * kStep + p * 8;
-  uint32_t c[8], e[8];
+  const int in_step = lane % (kStep / kElems) * kElems, b = in_step / kBlock;
+  const int k = (int)(unit % o.steps) * kStep + in_step;
+  uint32_t c[kTurns], e[kTurns];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int s = lane / 32 + 2 * i;
-    c[i] = *reinterpret_cast<const uint32_t*>(o.codes + (unit * 8 + b) * 256 + s * 16 + p % 4 * 4);
+  for (int i = 0; i < kTurns; ++i) {
+    const int s = lane / (kStep / kElems) + kAtOnce * i;
+    const uint8_t* const at = o.codes + (unit * 8 + b) * 256 + s * 16 + in_step % kBlock / 2;
+    c[i] = kElems == 8 ? *reinterpret_cast<const uint32_t*>(at) : (uint32_t)*reinterpret_cast<const uint16_t*>(at);
     e[i] = o.scales[unit * kScaleBytes + b % 2 * 64 + s * 4 + b / 2];
   }
-  if (k >= K) return;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int64_t row = g * kGroup + lane / 32 + 2 * i;
-    if (row >= rows) return;
-    const float scale = scale_of(e[i]);
-    const bool nan = e[i] == 255u;
-    uint8_t* const dst = out + row * K * T::kBytes;
-    if constexpr (T::kBytes == 4) {
-      float f[8];
-      values_of(c[i], scale, nan, f);
-      u32x4 lo, hi;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        lo[j] = __builtin_bit_cast(uint32_t, f[j]);
-        hi[j] = __builtin_bit_cast(uint32_t, f[4 + j]);
-      }
-      store_vector<T>(dst, k, K, lo);
-      store_vector<T>(dst, k + 4, K, hi);
-    } else {
-      store_vector<T>(dst, k, K, packed_values<T>(c[i], scale, nan));
-    }
+  for (int i = 0; i < kTurns; ++i) {
+    const int64_t row = g * kGroup + lane / (kStep / kElems) + kAtOnce * i;
+    if (row < rows)
+      store_vector<T, kStream>(out + row * K * T::kBytes, k, K, packed_values<T>(c[i], scale_of(e[i]), e[i] == 255u));
   }
 }
 
@@ -205,13 +192,17 @@ hipError_t launch_quantize(const void* x, int type, int rows, int K, int64_t str
   }
 }
 
+template <class T>
+static hipError_t launch_dequantize_of(const Operand& o, int rows, int K, void* out, hipStream_t s) {
+  return launch_kernel(streams(out, K, T::kBytes) ? dequantize_kernel<T, true> : dequantize_kernel<T, false>,
+                       dim3(unit_blocks(o)), dim3(kWave * kWaves), 0, s, o, rows, K, static_cast<uint8_t*>(out));
+}
+
 hipError_t launch_dequantize(const Operand& o, int rows, int K, int type, void* out, hipStream_t s) {
-  const dim3 grid(unit_blocks(o)), block(kWave * kWaves);
-  uint8_t* const dst = static_cast<uint8_t*>(out);
   switch (type) {
-    case APT_TYPE_FP16: return launch_kernel(dequantize_kernel<Half>, grid, block, 0, s, o, rows, K, dst);
-    case APT_TYPE_BF16: return launch_kernel(dequantize_kernel<Bf16>, grid, block, 0, s, o, rows, K, dst);
-    default: return launch_kernel(dequantize_kernel<Float>, grid, block, 0, s, o, rows, K, dst);
+    case APT_TYPE_FP16: return launch_dequantize_of<Half>(o, rows, K, out, s);
+    case APT_TYPE_BF16: return launch_dequantize_of<Bf16>(o, rows, K, out, s);
+    default: return launch_dequantize_of<Float>(o, rows, K, out, s);
   }
 }
 

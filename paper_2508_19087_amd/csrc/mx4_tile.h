@@ -255,36 +255,40 @@ __global__ __launch_bounds__(kTileWaves* kWave, (MB * NB >= 12 ? 1 : 2)) void ti
   constexpr int kCols = T::kBytes == 4 ? 32 : NB * 32;  // columns of a pass
   constexpr int kRowPieces = kCols * T::kBytes / 16;    // 16-byte pieces of a row
   constexpr int kRowsAtOnce = kWave / kRowPieces;
+  auto epilogue = [&](auto kStream) __attribute__((always_inline)) {
 #pragma unroll
-  for (int a = 0; a < MB; ++a) {
+    for (int a = 0; a < MB; ++a) {
 #pragma unroll
-    for (int b0 = 0; b0 < NB; b0 += kCols / 32) {
-      if ((int64_t)m0 * (MB * 32) + a * 32 >= p.M || nw + b0 * 32 >= p.N) continue;  // uniform: no output here
+      for (int b0 = 0; b0 < NB; b0 += kCols / 32) {
+        if ((int64_t)m0 * (MB * 32) + a * 32 >= p.M || nw + b0 * 32 >= p.N) continue;  // uniform: no output here
 #pragma unroll
-      for (int b = b0; b < b0 + kCols / 32; ++b)
+        for (int b = b0; b < b0 + kCols / 32; ++b)
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          uint8_t* const at = slot + r * kStride + ((b - b0) * 32 + g * 8 + h * 4) * T::kBytes;
-          const v16f& c = acc[b][a];
-          if constexpr (T::kBytes == 4)
-            *reinterpret_cast<v4f*>(at) = v4f{c[g * 4], c[g * 4 + 1], c[g * 4 + 2], c[g * 4 + 3]};
-          else
-            *reinterpret_cast<u32x2*>(at) = join4<T>(c[g * 4], c[g * 4 + 1], c[g * 4 + 2], c[g * 4 + 3]);
+          for (int g = 0; g < 4; ++g) {
+            uint8_t* const at = slot + r * kStride + ((b - b0) * 32 + g * 8 + h * 4) * T::kBytes;
+            const v16f& c = acc[b][a];
+            if constexpr (T::kBytes == 4)
+              *reinterpret_cast<v4f*>(at) = v4f{c[g * 4], c[g * 4 + 1], c[g * 4 + 2], c[g * 4 + 3]};
+            else
+              *reinterpret_cast<u32x2*>(at) = join4<T>(c[g * 4], c[g * 4 + 1], c[g * 4 + 2], c[g * 4 + 3]);
+          }
+        __builtin_amdgcn_s_waitcnt(0xc07f);  // this wave's LDS writes are done
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int j = 0; j < 32 / kRowsAtOnce; ++j) {
+          const int row = j * kRowsAtOnce + lane / kRowPieces, piece = lane % kRowPieces;
+          const u32x4 v = *reinterpret_cast<const u32x4*>(slot + row * kStride + piece * 16);
+          const int64_t m = (int64_t)m0 * (MB * 32) + a * 32 + row;
+          const int n = nw + b0 * 32 + piece * T::kVec;
+          if (m < p.M) store_vector<T, kStream.value>(p.c + m * p.N * T::kBytes, n, p.N, v);
         }
-      __builtin_amdgcn_s_waitcnt(0xc07f);  // this wave's LDS writes are done
-      __builtin_amdgcn_wave_barrier();
-#pragma unroll
-      for (int j = 0; j < 32 / kRowsAtOnce; ++j) {
-        const int row = j * kRowsAtOnce + lane / kRowPieces, piece = lane % kRowPieces;
-        const u32x4 v = *reinterpret_cast<const u32x4*>(slot + row * kStride + piece * 16);
-        const int64_t m = (int64_t)m0 * (MB * 32) + a * 32 + row;
-        const int n = nw + b0 * 32 + piece * T::kVec;
-        if (m < p.M) store_vector<T>(p.c + m * p.N * T::kBytes, n, p.N, v);
+        __builtin_amdgcn_s_waitcnt(0xc07f);  // reads done before the slot is rewritten
+        __builtin_amdgcn_wave_barrier();
       }
-      __builtin_amdgcn_s_waitcnt(0xc07f);  // reads done before the slot is rewritten
-      __builtin_amdgcn_wave_barrier();
     }
-  }
+  };
+  if (streams(p.c, p.N, T::kBytes)) epilogue(std::true_type{});
+  else epilogue(std::false_type{});
 }
 
 }  // namespace mx4

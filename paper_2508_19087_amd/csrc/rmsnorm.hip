@@ -155,8 +155,8 @@ struct CodeScale {
 
 // T: element type; NV: vectors of 8 elements held per thread (0: none, the row
 // is read again in each pass); kCodes: q-bit codes, else MX4; kWhole: K is a
-// multiple of 8, so that no vector is cut by the row's end, and every row that is
-// read starts at a multiple of 4 bytes.
+// multiple of 8, so that no vector is cut by the row's end, and every row starts
+// at a multiple of 4 bytes where it is read and of 16 where it is written.
 template <class T, int NV, bool kCodes, bool kWhole>
 __global__ __launch_bounds__(kWave* kMaxWaves) void rmsnorm_kernel(NormArgs a) {
   __shared__ double lds_sum[kMaxWaves];
@@ -181,8 +181,9 @@ __global__ __launch_bounds__(kWave* kMaxWaves) void rmsnorm_kernel(NormArgs a) {
     else return load_near<T, true>(p, k, K);
   };
   auto settled = [&](u32x4 v, int k) __attribute__((always_inline)) { return kWhole ? v : settle<T>(v, k, K); };
+  // (h goes past the cache where the row stays in registers and is not read back)
   auto store = [&](uint8_t* p, int k, u32x4 v) __attribute__((always_inline)) {
-    if (kWhole && k < K) *reinterpret_cast<any_u32x4*>(p + (int64_t)k * 2) = v;
+    if (kWhole && k < K) store_bytes<2, (NV > 0)>(p + (int64_t)k * 2, 16, v);
     if (!kWhole) store_vector<T>(p, k, K, v);
   };
   // (0 * an infinite or NaN factor: the elements behind K stay 0)
@@ -325,7 +326,7 @@ __global__ __launch_bounds__(kWave* kMaxWaves) void rmsnorm_kernel(NormArgs a) {
 
 // (2 code + 1) scale, eight elements of a row per thread: bound by memory, 1
 // byte in and 2 or 4 out per element.
-template <class T>
+template <class T, bool kStream>
 __global__ __launch_bounds__(256) void dequantize_codes_kernel(const int8_t* __restrict__ codes,
                                                                const uint16_t* __restrict__ scale, int K, int parts,
                                                                uint8_t* __restrict__ out) {
@@ -348,6 +349,7 @@ __global__ __launch_bounds__(256) void dequantize_codes_kernel(const int8_t* __r
   for (int i = 0; i < 8; ++i) f[i] = (float)(2 * (int)(int8_t)(c[i / 4] >> (8 * (i % 4))) + 1) * s;
   uint8_t* const dst = out + row * K * T::kBytes;
   if constexpr (T::kBytes == 4) {
+    // (halves of 32 bytes a lane fill their lines in the cache)
     u32x4 lo, hi;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -357,7 +359,7 @@ __global__ __launch_bounds__(256) void dequantize_codes_kernel(const int8_t* __r
     store_vector<T>(dst, k, K, lo);
     store_vector<T>(dst, k + 4, K, hi);
   } else {
-    store_vector<T>(dst, k, K, join<T>(f));
+    store_vector<T, kStream>(dst, k, K, join<T>(f));
   }
 }
 
@@ -380,8 +382,8 @@ template <class T, bool kCodes>
 hipError_t launch_norm_of(const NormArgs& a, int64_t rows, hipStream_t s) {
   uintptr_t at = reinterpret_cast<uintptr_t>(a.x) | reinterpret_cast<uintptr_t>(a.gain) | (uintptr_t)(a.x_stride * 2);
   if (a.residual != nullptr) at |= reinterpret_cast<uintptr_t>(a.residual) | (uintptr_t)(a.r_stride * 2);
-  return a.K % 8 == 0 && at % 4 == 0 ? launch_norm_as<T, kCodes, true>(a, rows, s)
-                                     : launch_norm_as<T, kCodes, false>(a, rows, s);
+  return at % 4 == 0 && streams(a.h, a.K, 2) && streams(a.y, a.K, 2) ? launch_norm_as<T, kCodes, true>(a, rows, s)
+                                                                      : launch_norm_as<T, kCodes, false>(a, rows, s);
 }
 
 // A launch holds fewer than 2^32 threads: at 1024 a row, this many rows (whole
@@ -436,11 +438,18 @@ hipError_t launch_dequantize_codes(const int8_t* codes, const uint16_t* scale, i
     const dim3 grid((unsigned)(rows * parts)), block(256);
     const int8_t* const c = codes + r0 * K;
     uint8_t* const o = static_cast<uint8_t*>(out) + r0 * K * size;
+    const bool stream = streams(o, K, size);
     hipError_t e;
     switch (type) {
-      case APT_TYPE_FP16: e = launch_kernel(dequantize_codes_kernel<Half>, grid, block, 0, s, c, scale + r0, K, parts, o); break;
-      case APT_TYPE_BF16: e = launch_kernel(dequantize_codes_kernel<Bf16>, grid, block, 0, s, c, scale + r0, K, parts, o); break;
-      default: e = launch_kernel(dequantize_codes_kernel<Float>, grid, block, 0, s, c, scale + r0, K, parts, o); break;
+      case APT_TYPE_FP16:
+        e = launch_kernel(stream ? dequantize_codes_kernel<Half, true> : dequantize_codes_kernel<Half, false>, grid, block,
+                          0, s, c, scale + r0, K, parts, o);
+        break;
+      case APT_TYPE_BF16:
+        e = launch_kernel(stream ? dequantize_codes_kernel<Bf16, true> : dequantize_codes_kernel<Bf16, false>, grid, block,
+                          0, s, c, scale + r0, K, parts, o);
+        break;
+      default: e = launch_kernel(dequantize_codes_kernel<Float, false>, grid, block, 0, s, c, scale + r0, K, parts, o); break;
     }
     if (e != hipSuccess) return e;
   }
