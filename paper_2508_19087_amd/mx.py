@@ -287,30 +287,32 @@ def _norm_inputs(x, gain, residual, h, stream, where):
     """Checked inputs of a norm: x, the residual, the gain, h (given, or made where there is a residual,
     or None) and the C arguments up to the gain."""
     torch = _torch()
-    dtype = x.dtype
-    if dtype is not torch.float16 and dtype is not torch.bfloat16:
+    dtype, device = x.dtype, x.device
+    t = APT_TYPE_FP16 if dtype is torch.float16 else APT_TYPE_BF16 if dtype is torch.bfloat16 else 0
+    if not t:
         _refuse(where, "fp16 or bf16 rows are wanted")
     x, xs = _rows(x, where, stream)
-    M, K = x.shape
+    shape = x.shape
+    M, K = shape
     rp, rs, gp = None, 0, None
     if residual is not None:
-        if residual.shape != x.shape or residual.dtype is not dtype or residual.device != x.device:
+        if residual.dtype is not dtype or residual.shape != shape or residual.device != device:
             _refuse(where, "a residual like x is wanted")
         residual, rs = _rows(residual, where, stream)
         rp = residual.data_ptr()
     if gain is not None:
-        if gain.dim() != 1 or gain.shape[0] != K or gain.dtype is not dtype or gain.device != x.device:
+        if gain.dtype is not dtype or gain.dim() != 1 or gain.shape[0] != K or gain.device != device:
             _refuse(where, "a gain of x's width, type and device is wanted")
         if not gain.is_contiguous():
             with _on_stream(stream):
                 gain = gain.contiguous()
         gp = gain.data_ptr()
     if h is not None:
-        if h.shape != x.shape or h.dtype is not dtype or h.device != x.device or not h.is_contiguous():
+        if h.dtype is not dtype or h.shape != shape or h.device != device or not h.is_contiguous():
             _refuse(where, "a contiguous h like x is wanted")
     elif residual is not None:
         h = _new_like(x, dtype, stream)
-    return x, residual, gain, h, (M, K, _type(dtype, where), x.data_ptr(), xs, rp, rs, gp)
+    return x, residual, gain, h, (M, K, t, x.data_ptr(), xs, rp, rs, gp)
 
 
 def rmsnorm_codes(x, gain, q: int, eps: float, residual=None, h=None, out_y: bool = False, stream=None):
