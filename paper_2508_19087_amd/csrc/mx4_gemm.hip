@@ -33,7 +33,7 @@ constexpr double kUnits = 256.0;  // compute units
 
 // Activations given as rows are quantized by the few-row kernel's workgroups
 // themselves, each on its own, up to this many elements (rows padded to steps).
-// One row of 4096 to 11008 columns: 6.1 us in a graph against 8.8 with a launch
+// One row of 4096 to 11008 columns: 6.1 us in a graph against 8.5 with a launch
 // before; the conversion then adds about 1 us per 4096 elements, so that 4 rows
 // of 4096 break even in a graph (9.6 against 8.9 us with 11008 columns, 5.7 and
 // 5.7 with 4096) and save a launch's 2 us of host time in a call by itself.
@@ -50,9 +50,9 @@ double per_step(double tiles, const Tile& t) {
 
 // The kernel of a problem: -1 for the few-row kernel, else an index into kTiles.
 // Up to 32 rows the few-row kernel is the faster everywhere (32 x 11008 x 4096
-// 7.2 us against 7.7, 32 x 4096 x 11008 6.8 against 14.7); from 65 on it does not
+// 6.8 us against 7.7, 32 x 4096 x 11008 6.6 against 14.7); from 65 on it does not
 // apply; between them the modelled times decide (64 x 11008 x 4096 9.9 against
-// 7.7 us on 32 x 128 tiles, 64 x 4096 x 11008 9.2 against 12.8).  Among the tiles
+// 7.7 us on 32 x 128 tiles, 64 x 4096 x 11008 8.8 against 12.8).  Among the tiles
 // a large one costs fewer loads per MFMA and a small one fills the chip:
 // 2048 x 11008 x 4096 takes 46 us at 128 x 256 and 59, 56, 64, 90 at 256 x 256,
 // 128, 64 and 32 x 128; 333 x 5003 x 2999 7.7 us at 64 x 128, 9.1 and 11.9 at 128 x

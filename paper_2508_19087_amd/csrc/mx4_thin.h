@@ -6,7 +6,14 @@
 // as 1 KB of the operand in lane order, and multiplies them with up to 16
 // activation rows.  A workgroup owns 16 weight rows; its waves take the steps of
 // K in turn, each issuing the loads of kAhead steps before it multiplies, and
-// add their sums through LDS in the order of the waves.
+// add their sums through LDS in the order of the waves.  Activations of an
+// operand come three steps ahead of their use (one step ahead: 1 x 11008 x 4096
+// 6.1 us instead of 5.8, 32 x 11008 x 4096 7.2 instead of 6.8), from LDS one.
+//
+// In a graph, a launch's 1.5 us included, 1 x 11008 x 4096 takes 5.8 us: its 24 MB
+// of weights pass at the rate of a large copy.  64 x 4096 x 11008 takes 8.8 us for
+// as many bytes: every workgroup reads all 375 KB of the activations from L2, and
+// with 16 columns to a compute unit that is three times what it reads of weights.
 //
 // The four scales of a lane's dword belong to blocks b, b + 2, b + 4, b + 6 of
 // the step; lane group q = lane / 16 multiplies blocks q and q + 4, bytes
@@ -20,7 +27,9 @@ namespace apt {
 namespace mx4 {
 
 constexpr int kThinRows = 64;  // activation rows, at most
-constexpr int kThinWaves = 4;  // waves of a workgroup (8 and 16 are slower, as 1 x 11008 x 4096: 6.0, 6.6, 9.4 us)
+// waves of a workgroup (1 x 11008 x 4096, activations a step ahead: 6.1 us, with 8
+// waves 6.6 and with 16 9.4)
+constexpr int kThinWaves = 4;
 constexpr int kAhead = 4;      // steps whose loads are in flight per wave
 
 // The MFMA of half j of a step.
@@ -106,6 +115,7 @@ template <int MT, class X>
 __global__ __launch_bounds__(kThinWaves* kWave) void thin_kernel(ThinParams p) {
   constexpr int KW = kThinWaves;
   constexpr bool kRows = !std::is_void<X>::value;
+  constexpr int DA = kRows ? 2 : 4;  // steps of activations held: kAhead is a multiple
   extern __shared__ __attribute__((aligned(16))) uint8_t rows_lds[];
   __shared__ float sums[KW][MT * 256];
   const int lane = threadIdx.x % kWave;
@@ -120,8 +130,8 @@ __global__ __launch_bounds__(kThinWaves* kWave) void thin_kernel(ThinParams p) {
   v4f acc[MT];
 #pragma unroll
   for (int i = 0; i < MT; ++i) acc[i] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-  u32x4 w[kAhead][2], a[2][MT][2];
-  uint32_t sw[kAhead], sa[2][MT];
+  u32x4 w[kAhead][2], a[DA][MT][2];
+  uint32_t sw[kAhead], sa[DA][MT];
   // (steps that are not there read the last one and are not multiplied)
   auto load_w = [&](int u, int t) __attribute__((always_inline)) {
     const int64_t at = min(t, S - 1);
@@ -172,17 +182,19 @@ __global__ __launch_bounds__(kThinWaves* kWave) void thin_kernel(ThinParams p) {
     lds_barrier();
     load_a(0, wave);
   } else {
-    load_a(0, wave);
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) load_w(u, wave + u * KW);
+    for (int u = 0; u < kAhead; ++u) {
+      if (u + 1 < DA) load_a(u, wave + u * KW);
+      load_w(u, wave + u * KW);
+    }
   }
   auto multiply = [&](int u) __attribute__((always_inline)) {
     const int x = (int)(sw[u] >> shift);
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
-      const int y = (int)(sa[u % 2][i] >> shift);
-      acc[i] = mfma16(w[u][0], a[u % 2][i][0], acc[i], 0, x, y);
-      acc[i] = mfma16(w[u][1], a[u % 2][i][1], acc[i], 1, x, y);
+      const int y = (int)(sa[u % DA][i] >> shift);
+      acc[i] = mfma16(w[u][0], a[u % DA][i][0], acc[i], 0, x, y);
+      acc[i] = mfma16(w[u][1], a[u % DA][i][1], acc[i], 1, x, y);
     }
   };
   // while steps follow: each multiplied step's registers take the loads of the
@@ -192,7 +204,7 @@ __global__ __launch_bounds__(kThinWaves* kWave) void thin_kernel(ThinParams p) {
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
       const int t = t0 + u * KW;
-      load_a((u + 1) % 2, t + KW);
+      load_a((u + DA - 1) % DA, t + (DA - 1) * KW);
       __builtin_amdgcn_sched_barrier(0);
       multiply(u);
       load_w(u, t + kAhead * KW);
@@ -202,7 +214,7 @@ __global__ __launch_bounds__(kThinWaves* kWave) void thin_kernel(ThinParams p) {
 #pragma unroll
   for (int u = 0; u < kAhead; ++u) {
     const int t = t0 + u * KW;
-    if (u + 1 < kAhead) load_a((u + 1) % 2, t + KW);
+    if (u + DA - 1 < kAhead) load_a((u + DA - 1) % DA, t + (DA - 1) * KW);
     __builtin_amdgcn_sched_barrier(0);
     if (t < S) multiply(u);
   }
