@@ -5,12 +5,16 @@
 // conversion instruction per two elements, which rounds to nearest even and
 // saturates) hides behind the loads.
 //
-// A wave takes 16 rows and one step (256 elements) of K: lane s + 16 q holds
-// blocks q and q + 4 of row s, whole blocks, so that a block's scale needs no
-// other lane, its 16 code bytes are one store, and the wave's stores are whole
-// 1 KB runs of the operand.  The lane's reads are 64 (or 128) contiguous bytes
-// in 16-byte pieces; the lines that a piece leaves unread are read by the
-// same wave's next pieces from the L1 cache.
+// A wave quantizes eight rows of one step (256 elements) of K: eight lanes to a
+// row, four to a block, eight elements to a lane.  A load instruction then reads
+// whole lines, two blocks of each row, a block's largest magnitude takes two lane
+// swaps, and the codes leave in runs of 128 bytes; a lane sees its block of all
+// four instructions, whose scales are one dword of the operand.  (With whole
+// blocks to a lane, a wave took 16 rows and each load touched 64 lines: 64 x 4096
+// fp16 3.4 us in a graph instead of 2.7, 2048 x 11008 bf16 11.1 instead of 10.1 and
+// fp32 23.7 instead of 17.8, which are 57 and 102 MB.)  Values take four rows of
+// a step per wave: 2048 x 11008 bf16 9.9 us and fp32 16.6 (16 rows: 10.3 and 17.3;
+// 64 x 4096 2.55 and 2.78 instead of 3.3 and 4.1).
 #include "mx4.h"
 
 namespace apt {
@@ -20,63 +24,65 @@ using namespace mx4;
 
 constexpr int kWave = 64;
 constexpr int kWaves = 4;
+constexpr int kQuantizeParts = 2, kValueParts = 4;  // waves to 16 rows of a step
 
 template <class T>
 __global__ __launch_bounds__(kWave* kWaves) void quantize_kernel(const uint8_t* __restrict__ x, int rows, int K,
                                                                  int64_t stride, Operand o) {
-  constexpr int kPieces = kBlock / T::kVec;
+  constexpr int kPieces = 8 / T::kVec;  // vectors of a lane's eight elements
   const int lane = threadIdx.x % kWave;
-  const int64_t unit = (int64_t)blockIdx.x * kWaves + threadIdx.x / kWave;
+  const int64_t at = (int64_t)blockIdx.x * kWaves + threadIdx.x / kWave;
+  const int64_t unit = at / kQuantizeParts;
   if (unit >= o.groups * o.steps) return;
-  const int s = lane % kGroup, q = lane / kGroup;
   const int64_t g = unit / o.steps;
-  const int k0 = (int)(unit % o.steps) * kStep;
+  const int first = (int)(at % kQuantizeParts) * (kGroup / kQuantizeParts);
+  if (g * kGroup + first >= rows) return;
+  const int s = first + lane / 8, h = lane / 4 % 2, e = lane % 4;
   const int64_t row = g * kGroup + s;
   const bool real = row < rows;
-  const uint8_t* const src = x + (real ? row : 0) * stride * T::kBytes;
-  u32x4 v[2][kPieces];
   // (rows past the edge read the first row and store nothing)
+  const uint8_t* const src = x + (real ? row : 0) * stride * T::kBytes;
+  const int k0 = (int)(unit % o.steps) * kStep;
+  u32x4 v[4][kPieces];
   const bool dwords = T::kBytes == 4 || ((reinterpret_cast<uintptr_t>(x) | (uintptr_t)(stride * 2)) & 3) == 0;
-  auto place = [&](int u, int i) __attribute__((always_inline)) { return k0 + (q + 4 * u) * kBlock + i * T::kVec; };
+  auto place = [&](int i, int j) __attribute__((always_inline)) { return k0 + i * 2 * kBlock + lane % 8 * 8 + j * T::kVec; };
   if (k0 + kStep <= K && dwords) {
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
+    for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int i = 0; i < kPieces; ++i) v[u][i] = load_whole<T>(src, place(u, i));
+      for (int j = 0; j < kPieces; ++j) v[i][j] = load_whole<T>(src, place(i, j));
   } else {
     if (dwords) {
 #pragma unroll
-      for (int u = 0; u < 2; ++u)
+      for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int i = 0; i < kPieces; ++i) v[u][i] = load_near<T, false>(src, place(u, i), K);
+        for (int j = 0; j < kPieces; ++j) v[i][j] = load_near<T, false>(src, place(i, j), K);
     } else {
 #pragma unroll
-      for (int u = 0; u < 2; ++u)
+      for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int i = 0; i < kPieces; ++i) v[u][i] = load_near<T, true>(src, place(u, i), K);
+        for (int j = 0; j < kPieces; ++j) v[i][j] = load_near<T, true>(src, place(i, j), K);
     }
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
+    for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int i = 0; i < kPieces; ++i) v[u][i] = settle<T>(v[u][i], place(u, i), K);
+      for (int j = 0; j < kPieces; ++j) v[i][j] = settle<T>(v[i][j], place(i, j), K);
   }
   uint32_t bytes = 0u;
 #pragma unroll
-  for (int u = 0; u < 2; ++u) {
+  for (int i = 0; i < 4; ++i) {
     uint32_t m = 0u;
 #pragma unroll
-    for (int i = 0; i < kPieces; ++i) m = fold_magnitude<T>(m, v[u][i]);
-    const uint32_t byte = scale_byte<T>(widest<T>(m));
-    const float scale = scale_of(byte);
-    u32x4 c;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) c[i] = byte == 255u ? 0u : codes_of<T>(v[u] + i * kPieces / 4, scale);
-    if (real) *reinterpret_cast<u32x4*>(o.codes + (unit * 8 + q + 4 * u) * 256 + s * 16) = c;
-    bytes |= byte << (16 * u);
+    for (int j = 0; j < kPieces; ++j) m = fold_magnitude<T>(m, v[i][j]);
+    m = widest<T>(m);
+    m = max(m, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0xB1, 0xF, 0xF, false));  // lane ^ 1
+    m = max(m, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0x4E, 0xF, 0xF, false));  // lane ^ 2
+    const uint32_t byte = scale_byte<T>(m);
+    const uint32_t c = byte == 255u ? 0u : codes_of<T>(v[i], scale_of(byte));
+    if (real) *reinterpret_cast<uint32_t*>(o.codes + (unit * 8 + 2 * i + h) * 256 + s * 16 + e * 4) = c;
+    bytes |= byte << (8 * i);
   }
-  // blocks q, q + 4 are bytes 0, 2 (q < 2) or 1, 3 of the dword of half q mod 2
-  bytes |= (uint32_t)__shfl_xor((int)bytes, 32) << 8;
-  if (real && q < 2) *reinterpret_cast<uint32_t*>(o.scales + unit * kScaleBytes + q * 64 + s * 4) = bytes;
+  if (real && e == 0) *reinterpret_cast<uint32_t*>(o.scales + unit * kScaleBytes + h * 64 + s * 4) = bytes;
 }
 
 // A vector of values: of eight codes in 16-bit types, of four in fp32.
@@ -105,32 +111,34 @@ __device__ __forceinline__ u32x4 packed_values(uint32_t c, float scale, bool nan
   return v;
 }
 
-// Values of an operand.  A wave takes 16 rows and one step again; its lanes take
-// the elements of a row in order, eight at a time for 16-bit types (rows l / 32 +
-// 2 i) and four for fp32, so that every store instruction writes whole 512-byte
-// or 1 KB runs.
+// Values of an operand.  A wave takes four rows of a step; its lanes take the
+// elements of a row in order, eight at a time for 16-bit types (two rows at once)
+// and four for fp32, so that every store instruction writes whole 512-byte or
+// 1 KB runs.
 template <class T, bool kStream>
 __global__ __launch_bounds__(kWave* kWaves) void dequantize_kernel(Operand o, int rows, int K, uint8_t* __restrict__ out) {
   constexpr int kElems = T::kVec;                  // per lane and row
   constexpr int kAtOnce = kWave * kElems / kStep;  // rows per store
-  constexpr int kTurns = kGroup / kAtOnce;
+  constexpr int kTurns = kGroup / kAtOnce / kValueParts;
   const int lane = threadIdx.x % kWave;
-  const int64_t unit = (int64_t)blockIdx.x * kWaves + threadIdx.x / kWave;
+  const int64_t at = (int64_t)blockIdx.x * kWaves + threadIdx.x / kWave;
+  const int64_t unit = at / kValueParts;
   if (unit >= o.groups * o.steps) return;
   const int64_t g = unit / o.steps;
+  const int first = (int)(at % kValueParts) * (kAtOnce * kTurns) + lane / (kStep / kElems);
   const int in_step = lane % (kStep / kElems) * kElems, b = in_step / kBlock;
   const int k = (int)(unit % o.steps) * kStep + in_step;
   uint32_t c[kTurns], e[kTurns];
 #pragma unroll
   for (int i = 0; i < kTurns; ++i) {
-    const int s = lane / (kStep / kElems) + kAtOnce * i;
-    const uint8_t* const at = o.codes + (unit * 8 + b) * 256 + s * 16 + in_step % kBlock / 2;
-    c[i] = kElems == 8 ? *reinterpret_cast<const uint32_t*>(at) : (uint32_t)*reinterpret_cast<const uint16_t*>(at);
+    const int s = first + kAtOnce * i;
+    const uint8_t* const from = o.codes + (unit * 8 + b) * 256 + s * 16 + in_step % kBlock / 2;
+    c[i] = kElems == 8 ? *reinterpret_cast<const uint32_t*>(from) : (uint32_t)*reinterpret_cast<const uint16_t*>(from);
     e[i] = o.scales[unit * kScaleBytes + b % 2 * 64 + s * 4 + b / 2];
   }
 #pragma unroll
   for (int i = 0; i < kTurns; ++i) {
-    const int64_t row = g * kGroup + lane / (kStep / kElems) + kAtOnce * i;
+    const int64_t row = g * kGroup + first + kAtOnce * i;
     if (row < rows)
       store_vector<T, kStream>(out + row * K * T::kBytes, k, K, packed_values<T>(c[i], scale_of(e[i]), e[i] == 255u));
   }
@@ -176,14 +184,14 @@ __global__ __launch_bounds__(256) void unpack_kernel(Operand o, int rows, int K,
   scales[row * blocks + k / kBlock] = o.scales[unit * kScaleBytes + b % 2 * 64 + s * 4 + b / 2];
 }
 
-unsigned unit_blocks(const Operand& o) { return (unsigned)((o.groups * o.steps + kWaves - 1) / kWaves); }
+unsigned unit_blocks(const Operand& o, int parts) { return (unsigned)((o.groups * o.steps * parts + kWaves - 1) / kWaves); }
 
 }  // namespace
 
 namespace mx4 {
 
 hipError_t launch_quantize(const void* x, int type, int rows, int K, int64_t stride, const Operand& o, hipStream_t s) {
-  const dim3 grid(unit_blocks(o)), block(kWave * kWaves);
+  const dim3 grid(unit_blocks(o, kQuantizeParts)), block(kWave * kWaves);
   const uint8_t* const src = static_cast<const uint8_t*>(x);
   switch (type) {
     case APT_TYPE_FP16: return launch_kernel(quantize_kernel<Half>, grid, block, 0, s, src, rows, K, stride, o);
@@ -195,7 +203,7 @@ hipError_t launch_quantize(const void* x, int type, int rows, int K, int64_t str
 template <class T>
 static hipError_t launch_dequantize_of(const Operand& o, int rows, int K, void* out, hipStream_t s) {
   return launch_kernel(streams(out, K, T::kBytes) ? dequantize_kernel<T, true> : dequantize_kernel<T, false>,
-                       dim3(unit_blocks(o)), dim3(kWave * kWaves), 0, s, o, rows, K, static_cast<uint8_t*>(out));
+                       dim3(unit_blocks(o, kValueParts)), dim3(kWave * kWaves), 0, s, o, rows, K, static_cast<uint8_t*>(out));
 }
 
 hipError_t launch_dequantize(const Operand& o, int rows, int K, int type, void* out, hipStream_t s) {
