@@ -33,11 +33,11 @@ constexpr double kUnits = 256.0;  // compute units
 
 // Activations given as rows are quantized by the few-row kernel's workgroups
 // themselves, each on its own, up to this many elements (rows padded to steps).
-// One row of 4096 to 11008 columns: 6.1 us in a graph against 8.5 with a launch
-// before; the conversion then adds about 1 us per 4096 elements, so that 4 rows
-// of 4096 break even in a graph (9.6 against 8.9 us with 11008 columns, 5.7 and
-// 5.7 with 4096) and save a launch's 2 us of host time in a call by itself.
-constexpr int64_t kFusedElements = 16384;
+// The conversion takes about 1 us per 4096 elements and saves a launch, which is
+// 1.5 us of a graph and 2 us of the host's time.  In a graph, fused and not: 1 x
+// 11008 x 4096 6.7 and 8.4 us, 2 x 11008 x 4096 8.0 and 8.5, 3 x 11008 x 4096 9.3 and
+// 8.6, 3 x 4096 x 4096 5.3 and 5.2, 4 x 4096 x 4096 6.2 and 5.3, 16 x 4096 x 512 4.5 and 4.9.
+constexpr int64_t kFusedElements = 12288;
 
 int64_t tiles_of(int M, int N, const Tile& t) {
   return ((int64_t)M + t.mb * 32 - 1) / (t.mb * 32) * (((int64_t)N + t.nb * 128 - 1) / (t.nb * 128));
