@@ -33,10 +33,10 @@ constexpr double kUnits = 256.0;  // compute units
 
 // Activations given as rows are quantized by the few-row kernel's workgroups
 // themselves, each on its own, up to this many elements (rows padded to steps).
-// The conversion takes about 1 us per 4096 elements and saves a launch, which is
-// 1.5 us of a graph and 2 us of the host's time.  In a graph, fused and not: 1 x
-// 11008 x 4096 6.7 and 8.4 us, 2 x 11008 x 4096 8.0 and 8.5, 3 x 11008 x 4096 9.3 and
-// 8.6, 3 x 4096 x 4096 5.3 and 5.2, 4 x 4096 x 4096 6.2 and 5.3, 16 x 4096 x 512 4.5 and 4.9.
+// The conversion takes 0.8 us per 4096 elements and saves a launch, which is 1.5 us
+// of a graph and 2 us of the host's time.  In a graph, fused and not: 1 x 11008 x
+// 4096 6.1 and 8.4 us, 2 x 11008 x 4096 6.9 and 8.5, 3 x 11008 x 4096 8.1 and 8.4, 3 x
+// 4096 x 4096 4.7 and 5.1, 4 x 4096 x 4096 about 5.3 both, 16 x 4096 x 512 4.0 and 4.9.
 constexpr int64_t kFusedElements = 12288;
 
 int64_t tiles_of(int M, int N, const Tile& t) {

@@ -73,16 +73,26 @@ struct RowShare {
   static constexpr int kHeld = 2, kPieces = 8 / X::kVec;
   u32x4 v[kHeld][kPieces];
 
-  __device__ __forceinline__ void load(const ThinParams& p, int i0) {
+  // x / d, exact for the few thousand groups of eight here: x + 0.5 stays 0.5 / d
+  // of the quotient away from an integer, the estimate of 1 / d 2^-22 of it.
+  static __device__ __forceinline__ int quotient(int x, int d) {
+    return (int)(((float)x + 0.5f) * __builtin_amdgcn_rcpf((float)d));
+  }
+  template <bool kSplit>
+  __device__ __forceinline__ void load_as(const ThinParams& p, int i0) {
     const int per_row = p.steps * (kStep / 8), all = per_row * p.M;
 #pragma unroll
     for (int i = 0; i < kHeld; ++i) {
       const int x = min(i0 + i * kThinWaves * kWave, all - 1);
-      const int m = x / per_row, k = (x - m * per_row) * 8;
+      const int m = quotient(x, per_row), k = (x - m * per_row) * 8;
       const uint8_t* const row = p.x + m * p.x_stride * X::kBytes;
 #pragma unroll
-      for (int j = 0; j < kPieces; ++j) v[i][j] = load_near<X, true>(row, k + j * X::kVec, p.K);
+      for (int j = 0; j < kPieces; ++j) v[i][j] = load_near<X, kSplit>(row, k + j * X::kVec, p.K);
     }
+  }
+  __device__ __forceinline__ void load(const ThinParams& p, int i0) {
+    if (X::kBytes == 4 || ((reinterpret_cast<uintptr_t>(p.x) | (uintptr_t)(p.x_stride * 2)) & 3) == 0) load_as<false>(p, i0);
+    else load_as<true>(p, i0);
   }
   __device__ __forceinline__ void store(const ThinParams& p, uint8_t* lds, int i0) {
     const int per_row = p.steps * (kStep / 8), all = per_row * p.M;
@@ -90,7 +100,7 @@ struct RowShare {
 #pragma unroll
     for (int i = 0; i < kHeld; ++i) {
       const int x = i0 + i * kThinWaves * kWave;
-      const int row = min(x, all - 1) / per_row, y = min(x, all - 1) - row * per_row;  // eighth y of the row
+      const int row = quotient(min(x, all - 1), per_row), y = min(x, all - 1) - row * per_row;  // eighth y of the row
 #pragma unroll
       for (int j = 0; j < kPieces; ++j) v[i][j] = settle<X>(v[i][j], y * 8 + j * X::kVec, p.K);
       uint32_t m = 0u;
