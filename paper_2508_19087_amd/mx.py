@@ -186,10 +186,22 @@ def _rows(x, where, stream):
 
 @dataclass
 class Mx4:
-    """An MX4 operand on the device: `rows` rows of K values."""
+    """An MX4 operand on the device: `rows` rows of K values in apt_mx4_bytes(rows, K) bytes (uint8)."""
     data: "object"
     rows: int
     K: int
+    _checked = None  # the data that _data_of has seen
+
+
+def _data_of(a, where):
+    """The data of an operand, checked the first time."""
+    d = a.data
+    if a._checked is not d:
+        n = (_lib or lib()).apt_mx4_bytes(a.rows, a.K)
+        if not (n and d.is_cuda and d.dtype is _torch().uint8 and d.is_contiguous() and d.numel() >= n):
+            _refuse(where, "an operand of %d rows of %d values is %d bytes (uint8) on the device" % (a.rows, a.K, n))
+        a._checked = d
+    return d
 
 
 def _new_mx4(rows, K, like, stream, where) -> Mx4:
@@ -197,7 +209,9 @@ def _new_mx4(rows, K, like, stream, where) -> Mx4:
     n = (_lib or lib()).apt_mx4_bytes(rows, K)
     if n == 0:
         _refuse(where, "%d rows of %d values" % (rows, K))
-    return Mx4(_new(like, n, _torch().uint8, stream), rows, K)
+    a = Mx4(_new(like, n, _torch().uint8, stream), rows, K)
+    a._checked = a.data
+    return a
 
 
 def mx4_quantize(x, stream=None) -> Mx4:
@@ -214,7 +228,7 @@ def mx4_dequantize(a: Mx4, dtype=None, stream=None):
     """The values of an MX4 operand, [rows][K] of `dtype` (by default bf16, which holds them all)."""
     dtype = _torch().bfloat16 if dtype is None else dtype
     t = _type(dtype, "mx4_dequantize")
-    data = a.data
+    data = _data_of(a, "mx4_dequantize")
     out = _new(data, (a.rows, a.K), dtype, stream)
     _call("apt_mx4_dequantize", data.device, stream, data.data_ptr(), a.rows, a.K, t, out.data_ptr())
     return out
@@ -238,9 +252,10 @@ def mx4_pack(codes, scales, K: int, stream=None) -> Mx4:
 
 def mx4_unpack(a: Mx4, stream=None):
     """(codes, scales) of an MX4 operand as mx4_pack takes them."""
-    codes = _new(a.data, (a.rows, -(-a.K // 2)), a.data.dtype, stream)
-    scales = _new(a.data, (a.rows, -(-a.K // 32)), a.data.dtype, stream)
-    _call("apt_mx4_unpack", a.data.device, stream, a.data.data_ptr(), a.rows, a.K, codes.data_ptr(), scales.data_ptr())
+    data = _data_of(a, "mx4_unpack")
+    codes = _new(data, (a.rows, -(-a.K // 2)), data.dtype, stream)
+    scales = _new(data, (a.rows, -(-a.K // 32)), data.dtype, stream)
+    _call("apt_mx4_unpack", data.device, stream, data.data_ptr(), a.rows, a.K, codes.data_ptr(), scales.data_ptr())
     return codes, scales
 
 
@@ -248,7 +263,7 @@ def mx4_gemm(a: Mx4, w: Mx4, dtype=None, stream=None):
     """C = A W^T of two MX4 operands, [a.rows][w.rows] of `dtype` (fp16 by default)."""
     dtype = _torch().float16 if dtype is None else dtype
     t = _type(dtype, "mx4_gemm")
-    ad, wd = a.data, w.data
+    ad, wd = _data_of(a, "mx4_gemm"), _data_of(w, "mx4_gemm")
     device, M, N, K = ad.device, a.rows, w.rows, a.K
     if K != w.K or wd.device != device:
         _refuse("mx4_gemm", "operands of %d and %d values a row on %s and %s" % (K, w.K, device, wd.device))
@@ -265,7 +280,7 @@ def mx4_gemm_act(x, w: Mx4, dtype=None, stream=None, workspace=None):
     M, K = x.shape
     dtype = x.dtype if dtype is None else dtype
     tx, t = _type(x.dtype, "mx4_gemm_act"), _type(dtype, "mx4_gemm_act")
-    device, wd = x.device, w.data
+    device, wd = x.device, _data_of(w, "mx4_gemm_act")
     if K != w.K or wd.device != device:
         _refuse("mx4_gemm_act", "rows of %d values on %s for weights of %d on %s" % (K, device, w.K, wd.device))
     N = w.rows

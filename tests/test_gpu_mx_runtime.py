@@ -197,3 +197,20 @@ def test_helpers_refuse():
             call()
         assert e.value.status == apt.APT_ERR_INVALID_ARG, i
     torch.cuda.synchronize()
+
+
+def test_operands_that_are_not_are_refused():
+    w = apt.mx4_quantize(torch.zeros(16, 256, dtype=torch.float16, device="cuda"))
+    x = torch.zeros(1, 256, dtype=torch.float16, device="cuda")
+    for bad in (apt.Mx4(w.data[:-1], 16, 256), apt.Mx4(w.data, 17, 256), apt.Mx4(w.data, 16, 257), apt.Mx4(w.data, 0, 256),
+                apt.Mx4(w.data.to(torch.int8), 16, 256), apt.Mx4(w.data.cpu(), 16, 256),
+                apt.Mx4(torch.zeros(2 * w.data.numel(), dtype=torch.uint8, device="cuda")[::2], 16, 256),
+                apt.Mx4(torch.zeros(w.data.numel() + 1, dtype=torch.uint8, device="cuda")[1:], 16, 256)):
+        for call in (lambda: apt.mx4_dequantize(bad), lambda: apt.mx4_unpack(bad), lambda: apt.mx4_gemm(w, bad),
+                     lambda: apt.mx4_gemm(bad, w), lambda: apt.mx4_gemm_act(x, bad)):
+            with pytest.raises(apt.AptError) as e:
+                call()
+            assert e.value.status == apt.APT_ERR_INVALID_ARG
+    # the operand's own bytes in a larger buffer are one
+    again = apt.Mx4(torch.cat([w.data, w.data])[:w.data.numel()], 16, 256)
+    assert torch.equal(apt.mx4_gemm_act(x, again), apt.mx4_gemm_act(x, w))

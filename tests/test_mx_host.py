@@ -130,3 +130,11 @@ def test_helpers_refuse_host_tensors_and_wrong_shapes():
         with pytest.raises(apt.AptError) as e:
             call()
         assert e.value.status == BAD
+
+
+def test_operands_in_host_memory_are_refused():
+    a = apt.Mx4(torch.zeros(apt.apt_mx4_bytes(2, 64), dtype=torch.uint8), 2, 64)
+    for call in (lambda: apt.mx4_dequantize(a), lambda: apt.mx4_unpack(a), lambda: apt.mx4_gemm(a, a)):
+        with pytest.raises(apt.AptError) as e:
+            call()
+        assert e.value.status == BAD
