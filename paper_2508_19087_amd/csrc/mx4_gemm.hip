@@ -55,7 +55,7 @@ double per_step(double tiles, const Tile& t) {
 // 7.7 us on 32 x 128 tiles, 64 x 4096 x 11008 8.8 against 12.8).  Among the tiles
 // a large one costs fewer loads per MFMA and a small one fills the chip:
 // 2048 x 11008 x 4096 takes 46 us at 128 x 256 and 59, 56, 64, 90 at 256 x 256,
-// 128, 64 and 32 x 128; 333 x 5003 x 2999 7.7 us at 64 x 128, 9.1 and 11.9 at 128 x
+// 128, 64 and 32 x 128; 333 x 5003 x 2999 7.3 us at 64 x 128, 9.1 and 11.9 at 128 x
 // 128 and 128 x 256; 1024 x 4096 x 11008 27 at 128 x 128 and 31 at 128 x 256.
 int kernel_of(int M, int N, int K) {
   if (M <= 32) return -1;

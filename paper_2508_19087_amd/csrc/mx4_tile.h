@@ -13,6 +13,15 @@
 // before its use.  One barrier per step, in its middle: it makes the next step's
 // stage visible early enough that the first fragments and scales of that step
 // are read before this one ends, and it frees the stage of the step before.
+//
+// 2048 x 11008 x 4096 (128 x 256 tiles, bf16 output) takes 46 to 47 us in a graph,
+// 3.9 to 4.0 PFLOP/s, 16384 cubed 1755 us or 5.0.  Its MFMAs alone take 34 us: with
+// all units at dense products of random codes the clock falls to 1.5 to 1.6 GHz.
+// The rest is the last, partly filled round, and the loads' way into the unit (66
+// bytes a ns); which tiles share their weights in the cache makes no difference.
+// With about a tile per unit the ends count: the first step begins when its own
+// loads have landed, not those of the three that follow (256 x 11008 x 4096 10.6
+// us instead of 11.2, 333 x 5003 x 2999 7.3 instead of 7.6).
 #pragma once
 
 #include <type_traits>
@@ -212,21 +221,32 @@ __global__ __launch_bounds__(kTileWaves* kWave, (MB * NB >= 12 ? 1 : 2)) void ti
     __builtin_amdgcn_sched_barrier(0);
   };
 
+  // The first loads, in the order of their use: step 0 begins when its own have
+  // landed.  Where a wave holds two steps of weights, those of step 0 come behind
+  // A of step 1, so that as many loads follow that as later (kSince).
+  auto first_a = [&](uint8_t* stage, int t) __attribute__((always_inline)) {
 #pragma unroll
-  for (int x = 0; x < kPieces; ++x) {
-    load_a(stage0, 0, x);
-    load_a(stage1, min(1, S - 1), x);
-    load_a(stage2, min(2, S - 1), x);
-  }
-#pragma unroll
-  for (int x = 0; x < WD - 1; ++x)
+    for (int x = 0; x < kPieces; ++x) load_a(stage, min(t, S - 1), x);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  auto first_w = [&](int t) __attribute__((always_inline)) {
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
-      sw_[x][b] = load_ws(min(x, S - 1), b);
+      sw_[t][b] = load_ws(min(t, S - 1), b);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) w_[x][b][i] = load_w(min(x, S - 1), b, i);
+      for (int i = 0; i < 4; ++i) w_[t][b][i] = load_w(min(t, S - 1), b, i);
     }
-  __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt 0, lgkmcnt 0
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  first_a(stage0, 0);
+  if constexpr (WD == 4) first_w(0);
+  first_a(stage1, 1);
+  first_w(WD == 4 ? 1 : 0);
+  first_a(stage2, 2);
+  if constexpr (WD == 4) first_w(2);
+  constexpr int kBehind = 2 * kPieces + (WD - 1) * 5 * NB;  // loads behind those of stage0
+  static_assert(kBehind < 64, "vmcnt counts to 63");
+  __builtin_amdgcn_s_waitcnt(0x0F70 | (kBehind & 15) | (kBehind >> 4) << 14);
   __builtin_amdgcn_s_barrier();
   af[0] = read_a(stage0, 0);
   af[1] = read_a(stage0, 1);
