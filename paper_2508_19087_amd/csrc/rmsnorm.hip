@@ -6,12 +6,14 @@
 // 17/32) of the operand out.  A row is one workgroup's and stays in registers
 // between its passes (sum of squares, largest magnitude of y, codes), each
 // thread holding NV vectors of 8 elements; rows longer than the registers
-// reach (NV = 0) are read again in each pass.
+// reach (NV = 0) are read again in each pass.  In a graph 2048 x 4096 into codes
+// takes 13.2 us (59 MB, 4.5 TB/s; a large copy 5.2), into MX4 12.3, 1 x 4096 3.3
+// and 3.0: a launch and one trip to memory.
 //
 // The sum of squares runs in fp64.  A quantizer is a step function, and a y
 // that moved by one rounding with the order of its row's sum would now and then
 // move a code; squares of 11-bit values and their sums are exact to 2^-53 here,
-// so the order never shows in f, and y and its codes follow from f by single
+// so the order all but never shows in f; y and its codes follow from f by single
 // IEEE operations.
 #include "mx4.h"
 #include "rowcode.h"
