@@ -63,7 +63,9 @@ apt_status_t apt_mx4_quantize(const void* x, int type, int rows, int K, int64_t 
                               void* stream);
 
 /* The values of an MX4 operand, row-major [rows][K] of `type` (rounded to
- * nearest even for fp16, whose range they may leave; exact for bf16 and fp32).
+ * nearest even for fp16; exact for bf16 and fp32; infinite past the type's range,
+ * in bf16 and fp32 some values of the scale bytes 253 and 254, which quantizing
+ * does not give).
  *   out  device, aligned to its element size
  * Errors as apt_mx4_quantize. */
 apt_status_t apt_mx4_dequantize(const void* mx, int rows, int K, int type, void* out, void* stream);
@@ -130,12 +132,12 @@ apt_status_t apt_mx4_gemm_act(int M, int N, int K, const void* x, int x_type, in
  *   h          device [M][K] row-major or NULL: receives h; it may be x or
  *              residual itself where that one's stride is K, and overlaps
  *              nothing else
- *   y          device [M][K] row-major or NULL: receives y
+ *   y          device [M][K] row-major or NULL: receives y; overlaps nothing else
  *   codes, scale  device int8 [M][K] and fp16 bits [M]
  *   mx         device, apt_mx4_bytes(M, K) bytes, 16-byte aligned
  * Errors: APT_ERR_INVALID_ARG for sizes < 1, q outside [1, 8], a stride < K, a
  * type other than the two, a negative or non-finite eps, NULL x, codes, scale or
- * mx, or misaligned pointers; APT_ERR_UNSUPPORTED for K > 2^30; APT_ERR_HIP. */
+ * mx, a y that is x, residual or h, or misaligned pointers; APT_ERR_UNSUPPORTED for K > 2^30; APT_ERR_HIP. */
 apt_status_t apt_rmsnorm_codes(int M, int K, int type, const void* x, int64_t x_stride,
                                const void* residual, int64_t residual_stride, const void* gain,
                                double eps, int q, void* h, void* y, int8_t* codes, uint16_t* scale,

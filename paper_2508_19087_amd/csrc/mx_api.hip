@@ -57,6 +57,7 @@ apt_status_t norm_check(int M, int K, int type, const void* x, int64_t x_stride,
   if (!(eps >= 0.0) || !isfinite(eps)) return APT_ERR_INVALID_ARG;
   if (!aligned(gain, 2) || !aligned(h, 2) || !aligned(y, 2)) return APT_ERR_INVALID_ARG;
   if (h != nullptr && ((h == x && x_stride != K) || (h == residual && residual_stride != K))) return APT_ERR_INVALID_ARG;
+  if (y != nullptr && (y == x || y == residual || y == h)) return APT_ERR_INVALID_ARG;
   return K > kMaxK ? APT_ERR_UNSUPPORTED : APT_OK;
 }
 

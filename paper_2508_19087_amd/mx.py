@@ -225,7 +225,7 @@ def mx4_quantize(x, stream=None) -> Mx4:
 
 
 def mx4_dequantize(a: Mx4, dtype=None, stream=None):
-    """The values of an MX4 operand, [rows][K] of `dtype` (by default bf16, which holds them all)."""
+    """The values of an MX4 operand, [rows][K] of `dtype` (by default bf16, which holds all that quantizing gives)."""
     dtype = _torch().bfloat16 if dtype is None else dtype
     t = _type(dtype, "mx4_dequantize")
     data = _data_of(a, "mx4_dequantize")

@@ -138,3 +138,9 @@ def test_operands_in_host_memory_are_refused():
         with pytest.raises(apt.AptError) as e:
             call()
         assert e.value.status == BAD
+
+
+@pytest.mark.parametrize("bad", [dict(y=P), dict(x=3 * P, y=P), dict(y=2 * P)])
+def test_norms_refuse_a_y_that_is_an_operand(bad):
+    assert apt.apt_rmsnorm_codes(**(NORM | dict(q=8, codes=P, scale=P) | bad)) == BAD
+    assert apt.apt_rmsnorm_mx4(**(NORM | dict(mx=P) | bad)) == BAD
