@@ -48,27 +48,46 @@ double per_step(double tiles, const Tile& t) {
   return load <= 1.0 ? t.few + (t.one - t.few) * load : t.share * std::ceil(load);
 }
 
-// The kernel of a problem: -1 for the few-row kernel, else an index into kTiles.
+// Workgroups of the few-row kernel at mt groups of 16 activation rows each.
+int64_t thin_blocks(int M, int N, int mt) { return ((int64_t)M + 16 * mt - 1) / (16 * mt) * groups(N); }
+
+// Its time in us.  A compute unit takes in about 105 bytes a ns, and a workgroup
+// reads 16 weight rows and 16 mt activation rows of 136 bytes a step; one alone is
+// bound by the loads' latency.  Weights from memory count by a third: the rest
+// hides.  Measured on 16 to 512 rows by 128 to 11008 columns, K = 1024 to 11008.
+double thin_time(int M, int N, int K, int mt) {
+  const double S = steps(K), load = (double)thin_blocks(M, N, mt) / kUnits;
+  const double few = 0.011 + 0.0175 * mt, one = 0.0207 * (mt + 1);
+  const double per = load <= 1.0 ? few + (one - few) * load : one * std::ceil(load);
+  return 2.4 + 0.05 * mt * std::ceil(load) + S * per + 0.3 * N * (double)K * 17 / 32 / 5.2e6;
+}
+
+// The kernel of a problem: -mt for the few-row kernel, else an index into kTiles.
 // Up to 32 rows the few-row kernel is the faster everywhere (32 x 11008 x 4096
-// 6.8 us against 7.7, 32 x 4096 x 11008 6.6 against 14.7); from 65 on it does not
-// apply; between them the modelled times decide (64 x 11008 x 4096 9.9 against
-// 7.7 us on 32 x 128 tiles, 64 x 4096 x 11008 8.8 against 12.8).  Among the tiles
-// a large one costs fewer loads per MFMA and a small one fills the chip:
+// 6.8 us against 7.7, 32 x 4096 x 11008 6.6 against 14.7); beyond, the modelled times
+// decide.  It wins where its 16 columns a workgroup fill the chip and the tiles' 128 do
+// not (64 x 512 x 11008 3.7 us at mt = 1, 4.6 and 6.5 at 2 and 4, tiles 9; 256 x 512 x
+// 11008 5.9 at mt = 2, tiles 11.9; 128 x 2048 x 11008 8.1 at mt = 4, tiles 12.3; 128 x 4096
+// x 11008 13.4 at mt = 4, tiles 12.6; 64 x 11008 x 4096 9.3 at mt = 4, tiles 7.2).  Among
+// the tiles a large one costs fewer loads per MFMA and a small one fills the chip:
 // 2048 x 11008 x 4096 takes 46 us at 128 x 256 and 59, 56, 64, 90 at 256 x 256,
 // 128, 64 and 32 x 128; 333 x 5003 x 2999 7.3 us at 64 x 128, 9.1 and 11.9 at 128 x
-// 128 and 128 x 256; 1024 x 4096 x 11008 27 at 128 x 128 and 31 at 128 x 256.
+// 128 and 128 x 256; 1024 x 4096 x 11008 25 at 128 x 128 and 31 at 128 x 256.
 int kernel_of(int M, int N, int K) {
-  if (M <= 32) return -1;
-  const double S = steps(K);
   int best = -1;
-  double least = M <= kThinRows ? S * std::max(0.17, 0.12 * (double)groups(N) / kUnits) - 0.5 : 1e30;
-  for (int i = 0; i < kNumTiles; ++i) {
-    const Tile& t = kTiles[i];
-    const double us = S * per_step((double)tiles_of(M, N, t), t) + t.fixed;
+  double least = thin_time(M, N, K, 1);
+  auto consider = [&](int kernel, double us) {
     if (us < least) {
       least = us;
-      best = i;
+      best = kernel;
     }
+  };
+  if (M > 16) consider(-2, thin_time(M, N, K, 2));
+  if (M <= 32) return best;
+  consider(-4, thin_time(M, N, K, 4));
+  for (int i = 0; i < kNumTiles; ++i) {
+    const Tile& t = kTiles[i];
+    consider(i, 1.9 + steps(K) * per_step((double)tiles_of(M, N, t), t) + t.fixed);
   }
   return best;
 }
@@ -95,11 +114,13 @@ hipError_t launch_tile_of(const GemmParams& p, int kernel, hipStream_t s) {
   }
 }
 
-hipError_t launch_thin(const ThinParams& p, hipStream_t s) {
-  const dim3 grid((unsigned)p.w.groups), block(kWave * kThinWaves);
-  if (p.M <= 16) return launch_kernel(thin_kernel<1, void>, grid, block, 0, s, p);
-  if (p.M <= 32) return launch_kernel(thin_kernel<2, void>, grid, block, 0, s, p);
-  return launch_kernel(thin_kernel<4, void>, grid, block, 0, s, p);
+hipError_t launch_thin(const ThinParams& p, int mt, hipStream_t s) {
+  const dim3 grid((unsigned)thin_blocks(p.M, p.N, mt)), block(kWave * kThinWaves);
+  switch (mt) {
+    case 1: return launch_kernel(thin_kernel<1, void>, grid, block, 0, s, p);
+    case 2: return launch_kernel(thin_kernel<2, void>, grid, block, 0, s, p);
+    default: return launch_kernel(thin_kernel<4, void>, grid, block, 0, s, p);
+  }
 }
 
 }  // namespace
@@ -108,12 +129,12 @@ namespace mx4 {
 
 int64_t gemm_tiles(int M, int N, int K) {
   const int k = kernel_of(M, N, K);
-  return k < 0 ? groups(N) : tiles_of(M, N, kTiles[k]);
+  return k < 0 ? thin_blocks(M, N, -k) : tiles_of(M, N, kTiles[k]);
 }
 
 hipError_t launch_gemm(int M, int N, int K, const Operand& a, const Operand& w, int type, void* c, hipStream_t s) {
   const int k = kernel_of(M, N, K);
-  if (k < 0) return launch_thin(ThinParams{M, N, type, w.steps, a, w, static_cast<uint8_t*>(c), nullptr, 0, K}, s);
+  if (k < 0) return launch_thin(ThinParams{M, N, type, w.steps, a, w, static_cast<uint8_t*>(c), nullptr, 0, K}, -k, s);
   const GemmParams p{M, N, a, w, static_cast<uint8_t*>(c), 0, 0};
   switch (type) {
     case APT_TYPE_FP16: return launch_tile_of<Half>(p, k, s);

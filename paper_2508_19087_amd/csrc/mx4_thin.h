@@ -1,14 +1,16 @@
-// mx4_thin.h - the product of two MX4 operands for few rows of activations, for
-// gfx950.
+// mx4_thin.h - the product of two MX4 operands for few rows of activations, or
+// of weights, for gfx950.
 //
-// With up to 64 rows the weights are the traffic, and the kernel is a stream of
+// With few rows the weights are the traffic, and the kernel is a stream of
 // them: v_mfma_scale_f32_16x16x128_f8f6f4 takes 16 weight rows and 128 elements
 // as 1 KB of the operand in lane order, and multiplies them with up to 16
-// activation rows.  A workgroup owns 16 weight rows; its waves take the steps of
-// K in turn, each issuing the loads of kAhead steps before it multiplies, and
-// add their sums through LDS in the order of the waves.  Activations of an
-// operand come three steps ahead of their use (one step ahead: 1 x 11008 x 4096
-// 6.1 us instead of 5.8, 32 x 11008 x 4096 7.2 instead of 6.8), from LDS one.
+// activation rows.  A workgroup owns 16 weight rows and up to 64 activation rows
+// (more rows are more workgroups: that fills the chip where both operands have few,
+// which tiles of 128 columns do not); its waves take the steps of K in turn, each
+// issuing the loads of kAhead steps before it multiplies, and add their sums
+// through LDS in the order of the waves.  Activations of an operand come three
+// steps ahead of their use (one step ahead: 1 x 11008 x 4096 6.1 us instead of 5.8,
+// 32 x 11008 x 4096 7.2 instead of 6.8), from LDS one.
 //
 // In a graph, a launch's 1.5 us included, 1 x 11008 x 4096 takes 5.8 us: its 24 MB
 // of weights pass at the rate of a large copy.  64 x 4096 x 11008 takes 8.8 us for
@@ -26,7 +28,6 @@
 namespace apt {
 namespace mx4 {
 
-constexpr int kThinRows = 64;  // activation rows, at most
 // waves of a workgroup (1 x 11008 x 4096, activations a step ahead: 6.1 us, with 8
 // waves 6.6 and with 16 9.4)
 constexpr int kThinWaves = 4;
@@ -119,7 +120,7 @@ struct RowShare {
   }
 };
 
-// MT: groups of 16 activation rows.  X: void for an operand, or the element type
+// MT: groups of 16 activation rows of a workgroup.  X: void for an operand, or the element type
 // of the rows that the workgroup quantizes into LDS itself (MT = 1).
 template <int MT, class X>
 __global__ __launch_bounds__(kThinWaves* kWave) void thin_kernel(ThinParams p) {
@@ -132,7 +133,8 @@ __global__ __launch_bounds__(kThinWaves* kWave) void thin_kernel(ThinParams p) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int s = lane % 16, q = lane / 16;
   const int S = p.steps;
-  const int64_t g = blockIdx.x;  // weight row group
+  const int64_t g = blockIdx.x % (unsigned)p.w.groups;             // weight row group
+  const int row0 = blockIdx.x / (unsigned)p.w.groups * (MT * 16);  // first activation row
   const uint8_t* const wc = p.w.codes + g * S * kCodeBytes + lane * 16;
   const uint8_t* const ws = p.w.scales + g * S * kScaleBytes + q % 2 * 64 + s * 4;
   const int shift = q / 2 * 8;
@@ -154,7 +156,7 @@ __global__ __launch_bounds__(kThinWaves* kWave) void thin_kernel(ThinParams p) {
   const uint8_t* as[MT];
 #pragma unroll
   for (int i = 0; i < MT; ++i) {
-    const int m = min(i * 16 + s, p.M - 1);
+    const int m = min(row0 + i * 16 + s, p.M - 1);
     if constexpr (kRows) {
       ac[i] = rows_lds + (q * p.M + m) * 16;
       as[i] = rows_lds + S * p.M * (kStep / 2) + (q % 2 * p.M + m) * 4;
@@ -233,7 +235,7 @@ __global__ __launch_bounds__(kThinWaves* kWave) void thin_kernel(ThinParams p) {
   for (int i = 0; i < MT; ++i) *reinterpret_cast<v4f*>(&sums[wave][i * 256 + s * 16 + q * 4]) = acc[i];
   lds_barrier();
   for (int x = threadIdx.x; x < MT * 256; x += KW * kWave) {
-    const int m = x / 16;
+    const int m = row0 + x / 16;
     const int64_t n = g * 16 + x % 16;
     float v = sums[0][x];
 #pragma unroll

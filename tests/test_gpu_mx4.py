@@ -261,3 +261,41 @@ def test_gemm_act_strides_and_bad_rows(M):
     wide[M - 1, 5 + K - 1] = float("inf")
     got = apt.mx4_gemm_act(wide[:, 5:5 + K], pw, torch.float32)
     assert torch.isnan(got[M - 1]).all() and torch.equal(got[:M - 1], want[:M - 1])
+
+
+# Ragged products of every kernel and tile, with one to four steps of 256 behind the last whole four.
+EVERY_KERNEL = [
+    (76, 35, 925), (35, 46, 1120), (59, 34, 1313), (106, 36, 535),              # 16 rows a workgroup
+    (35, 1416, 823), (33, 1434, 1121), (33, 1448, 1500), (1403, 34, 1548),      # 32
+    (33, 2815, 1796), (2917, 33, 2050), (2756, 36, 1360), (33, 2894, 1649),     # 64
+    (41, 2021, 776), (92, 158, 2), (46, 40, 316), (51, 494, 627),               # tiles of 32 x 128
+    (2876, 263, 796), (1280, 873, 1), (2775, 269, 261), (2781, 260, 565),       # 64 x 128
+    (193, 8422, 815), (733, 2730, 1), (205, 8401, 259), (193, 8200, 531),       # 128 x 128
+    (582, 6555, 771), (2583, 1575, 1), (449, 8292, 266), (520, 7237, 520),      # 128 x 256
+    (4000, 4090, 13000), (3999, 4085, 13200), (3900, 4001, 13400), (3970, 4095, 13700)]  # 256 x 256
+
+
+def small_sums(seed, R, K):
+    """An operand with scales of 1 or 2, made on the device, and its values in fp64."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    nibbles = torch.randint(0, 16, (R, K), dtype=torch.uint8, device="cuda", generator=g)
+    scales = torch.randint(127, 129, (R, -(-K // 32)), dtype=torch.uint8, device="cuda", generator=g)
+    even = torch.nn.functional.pad(nibbles, (0, K % 2))
+    levels = torch.tensor([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0], dtype=torch.float64, device="cuda")
+    values = levels[(nibbles & 7).long()] * (1 - 2 * (nibbles >> 3).double())
+    values = values * (scales.double() - 126).repeat_interleave(32, 1)[:, :K]
+    return apt.mx4_pack(even[:, ::2] | even[:, 1::2] << 4, scales, K), values
+
+
+@pytest.mark.parametrize("M,N,K", EVERY_KERNEL)
+def test_gemm_of_every_kernel(M, N, K):
+    """Every partial sum is a multiple of 1/4 below 144 * 13700 < 2^21, which fp32 holds: the outputs are its roundings."""
+    a, va = small_sums(M, M, K)
+    w, vw = small_sums(N + 1, N, K)
+    want = va @ vw.t().contiguous()
+    for kind in ("fp32", "bf16", "fp16"):
+        got = apt.mx4_gemm(a, w, TYPES[kind])
+        torch.cuda.synchronize()
+        # (an exact sum in fp32 rounds once; past fp16's range it is infinite)
+        assert torch.equal(got, want.float().to(TYPES[kind])), kind
