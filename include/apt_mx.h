@@ -96,7 +96,7 @@ apt_status_t apt_mx4_gemm(int M, int N, int K, const void* a_mx, const void* w_m
 
 /* C = A * W^T with the activations given unpacked and quantized inside the call
  * as apt_mx4_quantize does; the result equals that of apt_mx4_quantize followed
- * by apt_mx4_gemm, bit for bit.  Up to 16 rows of together 12288 elements (rows
+ * by apt_mx4_gemm, bit for bit.  Up to 16 rows of together 16384 elements (rows
  * padded to 256) are quantized by the product's kernel itself; others go through
  * the workspace.
  *   x, x_type, x_stride  as apt_mx4_quantize, M rows

@@ -34,10 +34,11 @@ constexpr double kUnits = 256.0;  // compute units
 // Activations given as rows are quantized by the few-row kernel's workgroups
 // themselves, each on its own, up to this many elements (rows padded to steps).
 // The conversion takes 0.8 us per 4096 elements and saves a launch, which is 1.5 us
-// of a graph and 2 us of the host's time.  In a graph, fused and not: 1 x 11008 x
-// 4096 6.1 and 8.4 us, 2 x 11008 x 4096 6.9 and 8.5, 3 x 11008 x 4096 8.1 and 8.4, 3 x
-// 4096 x 4096 4.7 and 5.1, 4 x 4096 x 4096 about 5.3 both, 16 x 4096 x 512 4.0 and 4.9.
-constexpr int64_t kFusedElements = 12288;
+// of a graph and 4 us of a call's time on the host.  Fused and not, in a graph: 1 x
+// 11008 x 4096 6.1 and 8.4 us, 2 x 11008 x 4096 6.9 and 8.5, 3 x 11008 x 4096 8.1 and 8.4,
+// 4 x 11008 x 4096 9.2 and 8.5 (called by itself 8.7 and 11.0), 4 x 4096 x 4096 5.4 and 5.2
+// (7.0 and 10.9), 6 x 4096 x 4096 7.2 and 5.4, 16 x 4096 x 1024 5.5 and 5.2 (7.1 and 11.1).
+constexpr int64_t kFusedElements = 16384;
 
 int64_t tiles_of(int M, int N, const Tile& t) {
   return ((int64_t)M + t.mb * 32 - 1) / (t.mb * 32) * (((int64_t)N + t.nb * 128 - 1) / (t.nb * 128));

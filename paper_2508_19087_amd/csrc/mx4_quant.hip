@@ -26,9 +26,20 @@ constexpr int kWave = 64;
 constexpr int kWaves = 4;
 constexpr int kQuantizeParts = 2, kValueParts = 4;  // waves to 16 rows of a step
 
+// (a struct: each argument of a launch takes its share of the host's time)
+struct Rows {
+  uint8_t* x;
+  int rows, K;
+  int64_t stride;  // elements
+  Operand o;
+};
+
 template <class T>
-__global__ __launch_bounds__(kWave* kWaves) void quantize_kernel(const uint8_t* __restrict__ x, int rows, int K,
-                                                                 int64_t stride, Operand o) {
+__global__ __launch_bounds__(kWave* kWaves) void quantize_kernel(Rows a) {
+  const uint8_t* const x = a.x;
+  const int rows = a.rows, K = a.K;
+  const int64_t stride = a.stride;
+  const Operand o = a.o;
   constexpr int kPieces = 8 / T::kVec;  // vectors of a lane's eight elements
   const int lane = threadIdx.x % kWave;
   const int64_t at = (int64_t)blockIdx.x * kWaves + threadIdx.x / kWave;
@@ -116,7 +127,10 @@ __device__ __forceinline__ u32x4 packed_values(uint32_t c, float scale, bool nan
 // and four for fp32, so that every store instruction writes whole 512-byte or
 // 1 KB runs.
 template <class T, bool kStream>
-__global__ __launch_bounds__(kWave* kWaves) void dequantize_kernel(Operand o, int rows, int K, uint8_t* __restrict__ out) {
+__global__ __launch_bounds__(kWave* kWaves) void dequantize_kernel(Rows a) {
+  uint8_t* const out = a.x;
+  const int rows = a.rows, K = a.K;
+  const Operand o = a.o;
   constexpr int kElems = T::kVec;                  // per lane and row
   constexpr int kAtOnce = kWave * kElems / kStep;  // rows per store
   constexpr int kTurns = kGroup / kAtOnce / kValueParts;
@@ -192,18 +206,18 @@ namespace mx4 {
 
 hipError_t launch_quantize(const void* x, int type, int rows, int K, int64_t stride, const Operand& o, hipStream_t s) {
   const dim3 grid(unit_blocks(o, kQuantizeParts)), block(kWave * kWaves);
-  const uint8_t* const src = static_cast<const uint8_t*>(x);
+  const Rows a{static_cast<uint8_t*>(const_cast<void*>(x)), rows, K, stride, o};  // (not written)
   switch (type) {
-    case APT_TYPE_FP16: return launch_kernel(quantize_kernel<Half>, grid, block, 0, s, src, rows, K, stride, o);
-    case APT_TYPE_BF16: return launch_kernel(quantize_kernel<Bf16>, grid, block, 0, s, src, rows, K, stride, o);
-    default: return launch_kernel(quantize_kernel<Float>, grid, block, 0, s, src, rows, K, stride, o);
+    case APT_TYPE_FP16: return launch_kernel(quantize_kernel<Half>, grid, block, 0, s, a);
+    case APT_TYPE_BF16: return launch_kernel(quantize_kernel<Bf16>, grid, block, 0, s, a);
+    default: return launch_kernel(quantize_kernel<Float>, grid, block, 0, s, a);
   }
 }
 
 template <class T>
 static hipError_t launch_dequantize_of(const Operand& o, int rows, int K, void* out, hipStream_t s) {
   return launch_kernel(streams(out, K, T::kBytes) ? dequantize_kernel<T, true> : dequantize_kernel<T, false>,
-                       dim3(unit_blocks(o, kValueParts)), dim3(kWave * kWaves), 0, s, o, rows, K, static_cast<uint8_t*>(out));
+                       dim3(unit_blocks(o, kValueParts)), dim3(kWave * kWaves), 0, s, Rows{static_cast<uint8_t*>(out), rows, K, K, o});
 }
 
 hipError_t launch_dequantize(const Operand& o, int rows, int K, int type, void* out, hipStream_t s) {

@@ -328,10 +328,18 @@ __global__ __launch_bounds__(kWave* kMaxWaves) void rmsnorm_kernel(NormArgs a) {
 
 // (2 code + 1) scale, eight elements of a row per thread: bound by memory, 1
 // byte in and 2 or 4 out per element.
+struct CodesArgs {
+  const int8_t* codes;
+  const uint16_t* scale;
+  int K, parts;
+  uint8_t* out;
+};
 template <class T, bool kStream>
-__global__ __launch_bounds__(256) void dequantize_codes_kernel(const int8_t* __restrict__ codes,
-                                                               const uint16_t* __restrict__ scale, int K, int parts,
-                                                               uint8_t* __restrict__ out) {
+__global__ __launch_bounds__(256) void dequantize_codes_kernel(CodesArgs a) {
+  const int8_t* const codes = a.codes;
+  const uint16_t* const scale = a.scale;
+  const int K = a.K, parts = a.parts;
+  uint8_t* const out = a.out;
   const int64_t row = blockIdx.x / (unsigned)parts;
   const int k = ((int)(blockIdx.x % (unsigned)parts) * 256 + (int)threadIdx.x) * 8;
   if (k >= K) return;
@@ -438,20 +446,19 @@ hipError_t launch_dequantize_codes(const int8_t* codes, const uint16_t* scale, i
   for (int64_t r0 = 0; r0 < M; r0 += most) {
     const int64_t rows = M - r0 < most ? M - r0 : most;
     const dim3 grid((unsigned)(rows * parts)), block(256);
-    const int8_t* const c = codes + r0 * K;
-    uint8_t* const o = static_cast<uint8_t*>(out) + r0 * K * size;
-    const bool stream = streams(o, K, size);
+    const CodesArgs a{codes + r0 * K, scale + r0, K, parts, static_cast<uint8_t*>(out) + r0 * K * size};
+    const bool stream = streams(a.out, K, size);
     hipError_t e;
     switch (type) {
       case APT_TYPE_FP16:
         e = launch_kernel(stream ? dequantize_codes_kernel<Half, true> : dequantize_codes_kernel<Half, false>, grid, block,
-                          0, s, c, scale + r0, K, parts, o);
+                          0, s, a);
         break;
       case APT_TYPE_BF16:
         e = launch_kernel(stream ? dequantize_codes_kernel<Bf16, true> : dequantize_codes_kernel<Bf16, false>, grid, block,
-                          0, s, c, scale + r0, K, parts, o);
+                          0, s, a);
         break;
-      default: e = launch_kernel(dequantize_codes_kernel<Float, false>, grid, block, 0, s, c, scale + r0, K, parts, o); break;
+      default: e = launch_kernel(dequantize_codes_kernel<Float, false>, grid, block, 0, s, a); break;
     }
     if (e != hipSuccess) return e;
   }
