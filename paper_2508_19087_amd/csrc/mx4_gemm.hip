@@ -49,46 +49,61 @@ double per_step(double tiles, const Tile& t) {
   return load <= 1.0 ? t.few + (t.one - t.few) * load : t.share * std::ceil(load);
 }
 
-// Workgroups of the few-row kernel at mt groups of 16 activation rows each.
-int64_t thin_blocks(int M, int N, int mt) { return ((int64_t)M + 16 * mt - 1) / (16 * mt) * groups(N); }
+// A workgroup of the few-row kernel: 16 mt activation rows by 16 nt weight rows, the
+// steps it holds of each, and its time in us: `fixed` and `turn` for its start and
+// end, alone and for each that a compute unit runs in turn; a step of 256 elements
+// costs `few` with few units busy (loads' latency), `one` with each running one,
+// and `share` with several (a unit takes in about 105 bytes a ns, and a step is
+// 2176 (mt + nt)).  Measured on 16 to 768 rows by 128 to 11008 columns, K = 1024 to
+// 11008.  (64 x 16 rows come behind 32 x 32 everywhere, 64 x 64 behind one of these
+// or a tile.)
+struct Thin {
+  int mt, nt, ka, da;
+  double fixed, turn, few, one, share;
+};
+constexpr Thin kThins[] = {
+    {1, 1, 4, 4, 2.4, 0.05, 0.028, 0.041, 0.041},
+    {2, 1, 4, 4, 2.4, 0.10, 0.046, 0.062, 0.062},
+    {2, 2, 4, 4, 2.7, 0.25, 0.067, 0.088, 0.083},
+    {4, 2, 2, 2, 3.6, 0.40, 0.100, 0.125, 0.115},
+};
+constexpr int kNumThins = sizeof(kThins) / sizeof(kThins[0]);
 
-// Its time in us.  A compute unit takes in about 105 bytes a ns, and a workgroup
-// reads 16 weight rows and 16 mt activation rows of 136 bytes a step; one alone is
-// bound by the loads' latency.  Weights from memory count by a third: the rest
-// hides.  Measured on 16 to 512 rows by 128 to 11008 columns, K = 1024 to 11008.
-double thin_time(int M, int N, int K, int mt) {
-  const double S = steps(K), load = (double)thin_blocks(M, N, mt) / kUnits;
-  const double few = 0.011 + 0.0175 * mt, one = 0.0207 * (mt + 1);
-  const double per = load <= 1.0 ? few + (one - few) * load : one * std::ceil(load);
-  return 2.4 + 0.05 * mt * std::ceil(load) + S * per + 0.3 * N * (double)K * 17 / 32 / 5.2e6;
+int64_t blocks_of(int M, int N, const Thin& t) {
+  return ((int64_t)M + 16 * t.mt - 1) / (16 * t.mt) * ((groups(N) + t.nt - 1) / t.nt);
 }
 
-// The kernel of a problem: -mt for the few-row kernel, else an index into kTiles.
+double thin_time(int M, int N, int K, const Thin& t) {
+  const double load = (double)blocks_of(M, N, t) / kUnits, turns = std::ceil(load);
+  return t.fixed + t.turn * turns + steps(K) * (load <= 1.0 ? t.few + (t.one - t.few) * load : t.share * turns);
+}
+
+// The kernel of a problem: an index into kThins, or kNumThins and more for kTiles.
 // Up to 32 rows the few-row kernel is the faster everywhere (32 x 11008 x 4096
 // 6.8 us against 7.7, 32 x 4096 x 11008 6.6 against 14.7); beyond, the modelled times
-// decide.  It wins where its 16 columns a workgroup fill the chip and the tiles' 128 do
-// not (64 x 512 x 11008 3.7 us at mt = 1, 4.6 and 6.5 at 2 and 4, tiles 9; 256 x 512 x
-// 11008 5.9 at mt = 2, tiles 11.9; 128 x 2048 x 11008 8.1 at mt = 4, tiles 12.3; 128 x 4096
-// x 11008 13.4 at mt = 4, tiles 12.6; 64 x 11008 x 4096 9.3 at mt = 4, tiles 7.2).  Among
+// decide.  It wins where tiles of 128 columns leave much of the chip idle (in us, the
+// four workgroups of kThins and the best tile: 64 x 512 x 11008 3.7, 4.6, 5.9, 8.3, 9;
+// 64 x 4096 x 11008 11.6, 9.3, 7.7, 10.1, 12.5; 256 x 1024 x 11008 10.0, 8.5, 7.4, 9.7, 12.3; 128 x
+// 4096 x 11008 19.1, 15.1, 11.4, 10.3, 12.5; 256 x 4096 x 11008 34, 26, 18.8, 15.8, 13.3).  Among
 // the tiles a large one costs fewer loads per MFMA and a small one fills the chip:
 // 2048 x 11008 x 4096 takes 46 us at 128 x 256 and 59, 56, 64, 90 at 256 x 256,
 // 128, 64 and 32 x 128; 333 x 5003 x 2999 7.3 us at 64 x 128, 9.1 and 11.9 at 128 x
 // 128 and 128 x 256; 1024 x 4096 x 11008 25 at 128 x 128 and 31 at 128 x 256.
 int kernel_of(int M, int N, int K) {
-  int best = -1;
-  double least = thin_time(M, N, K, 1);
+  int best = 0;
+  double least = thin_time(M, N, K, kThins[0]);
   auto consider = [&](int kernel, double us) {
     if (us < least) {
       least = us;
       best = kernel;
     }
   };
-  if (M > 16) consider(-2, thin_time(M, N, K, 2));
+  for (int i = 1; i < kNumThins; ++i)
+    if (M > 8 * kThins[i].mt) consider(i, thin_time(M, N, K, kThins[i]));
   if (M <= 32) return best;
-  consider(-4, thin_time(M, N, K, 4));
   for (int i = 0; i < kNumTiles; ++i) {
     const Tile& t = kTiles[i];
-    consider(i, 1.9 + steps(K) * per_step((double)tiles_of(M, N, t), t) + t.fixed);
+    consider(kNumThins + i, 1.9 + steps(K) * per_step((double)tiles_of(M, N, t), t) + t.fixed);
   }
   return best;
 }
@@ -115,12 +130,19 @@ hipError_t launch_tile_of(const GemmParams& p, int kernel, hipStream_t s) {
   }
 }
 
-hipError_t launch_thin(const ThinParams& p, int mt, hipStream_t s) {
-  const dim3 grid((unsigned)thin_blocks(p.M, p.N, mt)), block(kWave * kThinWaves);
-  switch (mt) {
-    case 1: return launch_kernel(thin_kernel<1, void>, grid, block, 0, s, p);
-    case 2: return launch_kernel(thin_kernel<2, void>, grid, block, 0, s, p);
-    default: return launch_kernel(thin_kernel<4, void>, grid, block, 0, s, p);
+template <int I>
+hipError_t launch_thin(const ThinParams& p, hipStream_t s) {
+  constexpr Thin t = kThins[I];
+  const dim3 grid((unsigned)blocks_of(p.M, p.N, t)), block(kWave * kThinWaves);
+  return launch_kernel(thin_kernel<t.mt, t.nt, t.ka, t.da, void>, grid, block, 0, s, p);
+}
+
+hipError_t launch_thin_of(const ThinParams& p, int kernel, hipStream_t s) {
+  switch (kernel) {
+    case 0: return launch_thin<0>(p, s);
+    case 1: return launch_thin<1>(p, s);
+    case 2: return launch_thin<2>(p, s);
+    default: return launch_thin<3>(p, s);
   }
 }
 
@@ -130,17 +152,18 @@ namespace mx4 {
 
 int64_t gemm_tiles(int M, int N, int K) {
   const int k = kernel_of(M, N, K);
-  return k < 0 ? thin_blocks(M, N, -k) : tiles_of(M, N, kTiles[k]);
+  return k < kNumThins ? blocks_of(M, N, kThins[k]) : tiles_of(M, N, kTiles[k - kNumThins]);
 }
 
 hipError_t launch_gemm(int M, int N, int K, const Operand& a, const Operand& w, int type, void* c, hipStream_t s) {
   const int k = kernel_of(M, N, K);
-  if (k < 0) return launch_thin(ThinParams{M, N, type, w.steps, a, w, static_cast<uint8_t*>(c), nullptr, 0, K}, -k, s);
+  if (k < kNumThins)
+    return launch_thin_of(ThinParams{M, N, type, w.steps, a, w, static_cast<uint8_t*>(c), nullptr, 0, K}, k, s);
   const GemmParams p{M, N, a, w, static_cast<uint8_t*>(c), 0, 0};
   switch (type) {
-    case APT_TYPE_FP16: return launch_tile_of<Half>(p, k, s);
-    case APT_TYPE_BF16: return launch_tile_of<Bf16>(p, k, s);
-    default: return launch_tile_of<Float>(p, k, s);
+    case APT_TYPE_FP16: return launch_tile_of<Half>(p, k - kNumThins, s);
+    case APT_TYPE_BF16: return launch_tile_of<Bf16>(p, k - kNumThins, s);
+    default: return launch_tile_of<Float>(p, k - kNumThins, s);
   }
 }
 
@@ -152,9 +175,9 @@ hipError_t launch_gemm_rows(int M, int N, int K, const void* x, int x_type, int6
   const dim3 grid((unsigned)w.groups), block(kWave * kThinWaves);
   const size_t lds = thin_lds_bytes(M, K);
   switch (x_type) {
-    case APT_TYPE_FP16: return launch_kernel(thin_kernel<1, Half>, grid, block, lds, s, p);
-    case APT_TYPE_BF16: return launch_kernel(thin_kernel<1, Bf16>, grid, block, lds, s, p);
-    default: return launch_kernel(thin_kernel<1, Float>, grid, block, lds, s, p);
+    case APT_TYPE_FP16: return launch_kernel(thin_kernel<1, 1, 4, 2, Half>, grid, block, lds, s, p);
+    case APT_TYPE_BF16: return launch_kernel(thin_kernel<1, 1, 4, 2, Bf16>, grid, block, lds, s, p);
+    default: return launch_kernel(thin_kernel<1, 1, 4, 2, Float>, grid, block, lds, s, p);
   }
 }
 

@@ -31,7 +31,6 @@ namespace mx4 {
 // waves of a workgroup (1 x 11008 x 4096, activations a step ahead: 6.1 us, with 8
 // waves 6.6 and with 16 9.4)
 constexpr int kThinWaves = 4;
-constexpr int kAhead = 4;      // steps whose loads are in flight per wave
 
 // The MFMA of half j of a step.
 __device__ __forceinline__ v4f mfma16(u32x4 w, u32x4 a, v4f c, int j, int sw, int sa) {
@@ -120,38 +119,51 @@ struct RowShare {
   }
 };
 
-// MT: groups of 16 activation rows of a workgroup.  X: void for an operand, or the element type
-// of the rows that the workgroup quantizes into LDS itself (MT = 1).
-template <int MT, class X>
+// MT, NT: groups of 16 activation and weight rows of a workgroup.  KA, DA: steps of
+// weights and of activations that a wave holds; KA is a multiple of DA.  X: void
+// for an operand, or the element type of the rows that the workgroup quantizes
+// into LDS itself (MT = 1).
+template <int MT, int NT, int KA, int DA, class X>
 __global__ __launch_bounds__(kThinWaves* kWave) void thin_kernel(ThinParams p) {
   constexpr int KW = kThinWaves;
   constexpr bool kRows = !std::is_void<X>::value;
-  constexpr int DA = kRows ? 2 : 4;  // steps of activations held: kAhead is a multiple
   extern __shared__ __attribute__((aligned(16))) uint8_t rows_lds[];
-  __shared__ float sums[KW][MT * 256];
+  __shared__ float sums[KW][MT * NT * 256];
   const int lane = threadIdx.x % kWave;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int s = lane % 16, q = lane / 16;
   const int S = p.steps;
-  const int64_t g = blockIdx.x % (unsigned)p.w.groups;             // weight row group
-  const int row0 = blockIdx.x / (unsigned)p.w.groups * (MT * 16);  // first activation row
-  const uint8_t* const wc = p.w.codes + g * S * kCodeBytes + lane * 16;
-  const uint8_t* const ws = p.w.scales + g * S * kScaleBytes + q % 2 * 64 + s * 4;
+  const unsigned across = ((unsigned)p.w.groups + NT - 1) / NT;
+  const int64_t g0 = (int64_t)(blockIdx.x % across) * NT;  // first weight row group
+  const int row0 = blockIdx.x / across * (MT * 16);        // first activation row
   const int shift = q / 2 * 8;
 
-  v4f acc[MT];
+  v4f acc[MT][NT];
 #pragma unroll
-  for (int i = 0; i < MT; ++i) acc[i] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-  u32x4 w[kAhead][2], a[DA][MT][2];
-  uint32_t sw[kAhead], sa[DA][MT];
-  // (steps that are not there read the last one and are not multiplied)
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int j = 0; j < NT; ++j) acc[i][j] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+  u32x4 w[KA][NT][2], a[DA][MT][2];
+  uint32_t sw[KA][NT], sa[DA][MT];
+  // (groups and rows that are not there read the last one: their sums are not
+  // stored; steps that are not there read the last one and are not multiplied)
+  const uint8_t* wc[NT];
+  const uint8_t* ws[NT];
+#pragma unroll
+  for (int j = 0; j < NT; ++j) {
+    const int64_t g = min(g0 + j, p.w.groups - 1);
+    wc[j] = p.w.codes + g * S * kCodeBytes + lane * 16;
+    ws[j] = p.w.scales + g * S * kScaleBytes + q % 2 * 64 + s * 4;
+  }
   auto load_w = [&](int u, int t) __attribute__((always_inline)) {
     const int64_t at = min(t, S - 1);
-    w[u][0] = *reinterpret_cast<const u32x4*>(wc + at * kCodeBytes);
-    w[u][1] = *reinterpret_cast<const u32x4*>(wc + at * kCodeBytes + 1024);
-    sw[u] = *reinterpret_cast<const uint32_t*>(ws + at * kScaleBytes);
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      w[u][j][0] = *reinterpret_cast<const u32x4*>(wc[j] + at * kCodeBytes);
+      w[u][j][1] = *reinterpret_cast<const u32x4*>(wc[j] + at * kCodeBytes + 1024);
+      sw[u][j] = *reinterpret_cast<const uint32_t*>(ws[j] + at * kScaleBytes);
+    }
   };
-  // (rows that are not there read the last one: their sums are not stored)
   const uint8_t* ac[MT];
   const uint8_t* as[MT];
 #pragma unroll
@@ -183,7 +195,7 @@ __global__ __launch_bounds__(kThinWaves* kWave) void thin_kernel(ThinParams p) {
     share.load(p, threadIdx.x);
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) load_w(u, wave + u * KW);
+    for (int u = 0; u < KA; ++u) load_w(u, wave + u * KW);
     __builtin_amdgcn_sched_barrier(0);
     share.store(p, rows_lds, threadIdx.x);
     const int all = S * (kStep / 8) * p.M;
@@ -195,52 +207,58 @@ __global__ __launch_bounds__(kThinWaves* kWave) void thin_kernel(ThinParams p) {
     load_a(0, wave);
   } else {
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
+    for (int u = 0; u < KA; ++u) {
       if (u + 1 < DA) load_a(u, wave + u * KW);
       load_w(u, wave + u * KW);
     }
   }
   auto multiply = [&](int u) __attribute__((always_inline)) {
-    const int x = (int)(sw[u] >> shift);
 #pragma unroll
-    for (int i = 0; i < MT; ++i) {
-      const int y = (int)(sa[u % DA][i] >> shift);
-      acc[i] = mfma16(w[u][0], a[u % DA][i][0], acc[i], 0, x, y);
-      acc[i] = mfma16(w[u][1], a[u % DA][i][1], acc[i], 1, x, y);
+    for (int j = 0; j < NT; ++j) {
+      const int x = (int)(sw[u][j] >> shift);
+#pragma unroll
+      for (int i = 0; i < MT; ++i) {
+        const int y = (int)(sa[u % DA][i] >> shift);
+        acc[i][j] = mfma16(w[u][j][0], a[u % DA][i][0], acc[i][j], 0, x, y);
+        acc[i][j] = mfma16(w[u][j][1], a[u % DA][i][1], acc[i][j], 1, x, y);
+      }
     }
   };
   // while steps follow: each multiplied step's registers take the loads of the
-  // step kAhead turns on
+  // step KA turns on
   int t0 = wave;
-  for (; t0 + KW * kAhead < S; t0 += KW * kAhead) {
+  for (; t0 + KW * KA < S; t0 += KW * KA) {
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
+    for (int u = 0; u < KA; ++u) {
       const int t = t0 + u * KW;
       load_a((u + DA - 1) % DA, t + (DA - 1) * KW);
       __builtin_amdgcn_sched_barrier(0);
       multiply(u);
-      load_w(u, t + kAhead * KW);
+      load_w(u, t + KA * KW);
       __builtin_amdgcn_sched_barrier(0);
     }
   }
 #pragma unroll
-  for (int u = 0; u < kAhead; ++u) {
+  for (int u = 0; u < KA; ++u) {
     const int t = t0 + u * KW;
-    if (u + DA - 1 < kAhead) load_a((u + DA - 1) % DA, t + (DA - 1) * KW);
+    if (u + DA - 1 < KA) load_a((u + DA - 1) % DA, t + (DA - 1) * KW);
     __builtin_amdgcn_sched_barrier(0);
     if (t < S) multiply(u);
   }
   // lane (s, q) holds weight rows 4 q + 0..3 of activation row s
 #pragma unroll
-  for (int i = 0; i < MT; ++i) *reinterpret_cast<v4f*>(&sums[wave][i * 256 + s * 16 + q * 4]) = acc[i];
-  lds_barrier();
-  for (int x = threadIdx.x; x < MT * 256; x += KW * kWave) {
-    const int m = row0 + x / 16;
-    const int64_t n = g * 16 + x % 16;
-    float v = sums[0][x];
+  for (int i = 0; i < MT; ++i)
 #pragma unroll
-    for (int k = 1; k < KW; ++k) v += sums[k][x];
-    if (m < p.M && n < p.N) store_output(p.c, p.type, m * (int64_t)p.N + n, v);
+    for (int j = 0; j < NT; ++j) *reinterpret_cast<v4f*>(&sums[wave][(i * NT + j) * 256 + s * 16 + q * 4]) = acc[i][j];
+  lds_barrier();
+  for (int x = threadIdx.x; x < MT * NT * 256; x += KW * kWave) {
+    const int r = x / (NT * 16), c = x % (NT * 16);
+    const int at = (r / 16 * NT + c / 16) * 256 + r % 16 * 16 + c % 16;
+    const int64_t n = g0 * 16 + c;
+    float v = sums[0][at];
+#pragma unroll
+    for (int k = 1; k < KW; ++k) v += sums[k][at];
+    if (row0 + r < p.M && n < p.N) store_output(p.c, p.type, (row0 + r) * (int64_t)p.N + n, v);
   }
 }
 
