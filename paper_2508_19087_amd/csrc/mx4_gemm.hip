@@ -23,7 +23,7 @@ struct Tile {
 };
 constexpr Tile kTiles[] = {
     {1, 1, 0.22, 0.25, 0.25, 0.0},  // 32 x 128
-    {2, 1, 0.25, 0.34, 0.31, 0.0},  // 64 x 128
+    {2, 1, 0.25, 0.34, 0.331, 0.0},  // 64 x 128
     {4, 1, 0.36, 0.50, 0.55, 0.0},  // 128 x 128
     {4, 2, 0.32, 1.00, 0.84, 0.0},  // 128 x 256
     {8, 2, 0.85, 1.60, 1.60, 4.0},  // 256 x 256, one workgroup per compute unit: its epilogue stands alone

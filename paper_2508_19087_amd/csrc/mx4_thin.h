@@ -1,21 +1,22 @@
 // mx4_thin.h - the product of two MX4 operands for few rows of activations, or
 // of weights, for gfx950.
 //
-// With few rows the weights are the traffic, and the kernel is a stream of
-// them: v_mfma_scale_f32_16x16x128_f8f6f4 takes 16 weight rows and 128 elements
-// as 1 KB of the operand in lane order, and multiplies them with up to 16
-// activation rows.  A workgroup owns 16 weight rows and up to 64 activation rows
-// (more rows are more workgroups: that fills the chip where both operands have few,
-// which tiles of 128 columns do not); its waves take the steps of K in turn, each
-// issuing the loads of kAhead steps before it multiplies, and add their sums
-// through LDS in the order of the waves.  Activations of an operand come three
-// steps ahead of their use (one step ahead: 1 x 11008 x 4096 6.1 us instead of 5.8,
-// 32 x 11008 x 4096 7.2 instead of 6.8), from LDS one.
+// v_mfma_scale_f32_16x16x128_f8f6f4 takes 16 weight rows and 128 elements as 1 KB
+// of the operand in lane order, and multiplies them with up to 16 activation rows.
+// A workgroup owns 16 or 32 weight rows and up to 64 activation rows; its waves
+// take the steps of K in turn, straight from memory into registers, and add their
+// sums through LDS in the order of the waves.  So a workgroup has no barrier
+// before its end and four times a tile's loads in flight for its outputs, and small
+// ones fill the chip where tiles of 128 columns do not.
 //
-// In a graph, a launch's 1.5 us included, 1 x 11008 x 4096 takes 5.8 us: its 24 MB
-// of weights pass at the rate of a large copy.  64 x 4096 x 11008 takes 8.8 us for
-// as many bytes: every workgroup reads all 375 KB of the activations from L2, and
-// with 16 columns to a compute unit that is three times what it reads of weights.
+// What it reads bounds it.  One row: the weights, 1 x 11008 x 4096 5.8 us in a graph
+// (a launch's 1.5 included), 24 MB at the rate of a large copy.  More rows: what a
+// compute unit takes in, about 105 bytes a ns, 64 x 4096 x 11008 7.6 us in blocks of
+// 32 x 32 (375 KB a unit), 8.8 in 64 x 16 (470 KB), 9.3 in 32 x 16.
+//
+// Activations of an operand come three steps ahead of their use where registers
+// allow (one step ahead: 1 x 11008 x 4096 6.1 us, 32 x 11008 x 4096 7.2 instead of
+// 6.8), from LDS one.
 //
 // The four scales of a lane's dword belong to blocks b, b + 2, b + 4, b + 6 of
 // the step; lane group q = lane / 16 multiplies blocks q and q + 4, bytes

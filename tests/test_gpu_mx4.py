@@ -265,10 +265,14 @@ def test_gemm_act_strides_and_bad_rows(M):
 
 # Ragged products of every kernel and tile, with one to four steps of 256 behind the last whole four.
 EVERY_KERNEL = [
-    (76, 35, 925), (35, 46, 1120), (59, 34, 1313), (106, 36, 535),              # 16 rows a workgroup
-    (35, 1416, 823), (33, 1434, 1121), (33, 1448, 1500), (1403, 34, 1548),      # 32
-    (33, 2815, 1796), (2917, 33, 2050), (2756, 36, 1360), (33, 2894, 1649),     # 64
-    (41, 2021, 776), (92, 158, 2), (46, 40, 316), (51, 494, 627),               # tiles of 32 x 128
+    (76, 35, 925), (35, 46, 1120), (59, 34, 1313), (106, 36, 535),              # workgroups of 16 x 16 (and the next)
+    (33, 2815, 1796), (2917, 33, 2050), (2756, 36, 1360), (33, 2894, 1649),
+    (35, 1416, 823), (33, 1434, 1121), (33, 1448, 1500), (1403, 34, 1548),      # 32 x 16 (and the next)
+    (41, 2021, 776), (92, 158, 2), (46, 40, 316), (51, 494, 627),
+    (33, 2769, 2852), (50, 2130, 2050), (2772, 34, 2318), (2857, 33, 2591),     # 32 x 32
+    (34, 5516, 4876), (33, 5462, 5322), (34, 5523, 5433), (33, 6248, 4641),     # 64 x 32
+    (127, 4001, 5000), (126, 4000, 4800), (128, 3990, 5300), (150, 3700, 10708),
+    (34, 2324, 788), (37, 30, 2), (35, 20, 290), (38, 1155, 526),               # tiles of 32 x 128
     (2876, 263, 796), (1280, 873, 1), (2775, 269, 261), (2781, 260, 565),       # 64 x 128
     (193, 8422, 815), (733, 2730, 1), (205, 8401, 259), (193, 8200, 531),       # 128 x 128
     (582, 6555, 771), (2583, 1575, 1), (449, 8292, 266), (520, 7237, 520),      # 128 x 256
