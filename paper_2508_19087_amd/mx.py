@@ -132,18 +132,24 @@ def _refuse(where, what):
     raise AptError(APT_ERR_INVALID_ARG, "%s: %s" % (where, what))
 
 
+_raw_stream = _device = None  # torch's, once it is there
+
+
 def _call(name, device, stream, *args):
     """The C function `name` of the arguments and the raw stream, on `device`."""
-    C = _torch()._C
+    global _raw_stream, _device
+    if _device is None:
+        C = _torch()._C
+        _raw_stream, _device = C._cuda_getCurrentRawStream, C._cuda_getDevice
     index = device.index
     if stream is None:
-        raw = C._cuda_getCurrentRawStream(index)
+        raw = _raw_stream(index)
     else:
         if stream.device != device:
             _refuse(name, "a stream of another device")
         raw = stream.cuda_stream
     f = getattr(_lib or lib(), name)
-    if C._cuda_getDevice() == index:
+    if _device() == index:
         status = f(*args, raw)
     else:
         with _torch().cuda.device(device):
@@ -162,10 +168,9 @@ def _new(like, shape, dtype, stream):
 
 def _new_like(x, dtype, stream):
     """A new contiguous tensor of x's shape, of the call's stream."""
-    torch = _torch()
     if stream is None:
         if x.is_contiguous():
-            return torch.empty_like(x, dtype=dtype)
+            return _torch().empty_like(x, dtype=dtype)
         return x.new_empty(x.shape, dtype=dtype)
     with _on_stream(stream):
         return x.new_empty(x.shape, dtype=dtype)
@@ -313,10 +318,13 @@ def _norm_inputs(x, gain, residual, h, stream, where):
     if residual is not None:
         if residual.dtype is not dtype or residual.shape != shape or residual.device != device:
             _refuse(where, "a residual like x is wanted")
-        residual, rs = _rows(residual, where, stream)
+        if residual.is_contiguous():
+            rs = K
+        else:
+            residual, rs = _rows(residual, where, stream)
         rp = residual.data_ptr()
     if gain is not None:
-        if gain.dtype is not dtype or gain.dim() != 1 or gain.shape[0] != K or gain.device != device:
+        if gain.dtype is not dtype or gain.dim() != 1 or gain.numel() != K or gain.device != device:
             _refuse(where, "a gain of x's width, type and device is wanted")
         if not gain.is_contiguous():
             with _on_stream(stream):
@@ -340,7 +348,7 @@ def rmsnorm_codes(x, gain, q: int, eps: float, residual=None, h=None, out_y: boo
     x, residual, gain, h, args = _norm_inputs(x, gain, residual, h, stream, "rmsnorm_codes")
     y = _new_like(x, x.dtype, stream) if out_y else None
     codes = _new_like(x, torch.int8, stream)
-    scale = _new(x, x.shape[0], torch.float16, stream)
+    scale = _new(x, args[0], torch.float16, stream)
     _call("apt_rmsnorm_codes", x.device, stream, *args, eps, q, None if h is None else h.data_ptr(),
           None if y is None else y.data_ptr(), codes.data_ptr(), scale.data_ptr())
     return (codes, scale, h, y) if out_y else (codes, scale, h)
@@ -351,7 +359,7 @@ def rmsnorm_mx4(x, gain, eps: float, residual=None, h=None, out_y: bool = False,
     # (copies that were made stay alive until the call has been enqueued)
     x, residual, gain, h, args = _norm_inputs(x, gain, residual, h, stream, "rmsnorm_mx4")
     y = _new_like(x, x.dtype, stream) if out_y else None
-    out = _new_mx4(x.shape[0], x.shape[1], x, stream, "rmsnorm_mx4")
+    out = _new_mx4(args[0], args[1], x, stream, "rmsnorm_mx4")
     _call("apt_rmsnorm_mx4", x.device, stream, *args, eps, None if h is None else h.data_ptr(),
           None if y is None else y.data_ptr(), out.data.data_ptr())
     return (out, h, y) if out_y else (out, h)
