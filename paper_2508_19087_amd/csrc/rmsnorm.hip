@@ -85,6 +85,24 @@ __device__ __forceinline__ double block_sum(double v, double* lds) {
   for (int w = 0; w < waves; ++w) sum += lds[w];
   return sum;
 }
+// The same over kLanes neighbouring lanes (16, 32, or 64: a wave).
+template <int kLanes>
+__device__ __forceinline__ double lanes_sum(double v) {
+  v = add_dpp<0xB1>(v);
+  v = add_dpp<0x4E>(v);
+  v = add_dpp<0x141>(v);
+  v = add_dpp<0x140>(v);
+  if (kLanes == 32) v += __shfl_xor(v, 16);
+  if (kLanes == 64) v = (lane_of(v, 0) + lane_of(v, 16)) + (lane_of(v, 32) + lane_of(v, 48));
+  return v;
+}
+template <int kLanes>
+__device__ __forceinline__ uint32_t lanes_max(uint32_t v) {
+  if (kLanes == 64) return rowcode::wave_max(v);
+#pragma unroll
+  for (int d = 1; d < kLanes; d *= 2) v = max(v, (uint32_t)__shfl_xor((int)v, d));
+  return v;
+}
 __device__ __forceinline__ uint32_t block_max(uint32_t v, uint32_t* lds) {
   v = rowcode::wave_max(v);
   const int waves = (int)blockDim.x / kWave;
@@ -156,19 +174,31 @@ struct CodeScale {
 };
 
 // T: element type; NV: vectors of 8 elements held per thread (0: none, the row
-// is read again in each pass); kCodes: q-bit codes, else MX4; kWhole: K is a
+// is read again in each pass); LANES: 0, or the lanes that a row takes, several
+// rows to a workgroup; kCodes: q-bit codes, else MX4; kWhole: K is a
 // multiple of 8, so that no vector is cut by the row's end, and every row starts
 // at a multiple of 4 bytes where it is read and of 16 where it is written.
-template <class T, int NV, bool kCodes, bool kWhole>
+template <class T, int NV, int LANES, bool kCodes, bool kWhole>
 __global__ __launch_bounds__(kWave* kMaxWaves) void rmsnorm_kernel(NormArgs a) {
   __shared__ double lds_sum[kMaxWaves];
   __shared__ uint32_t lds_max[kMaxWaves];
-  const int tid = threadIdx.x, K = a.K;
+  const int K = a.K;
+  const int tid = LANES ? threadIdx.x % LANES : threadIdx.x;
+  const int threads = LANES ? LANES : (int)blockDim.x;  // of the row
   // MX4: the 16 rows of a group share the operand's lines, and workgroups are
   // dealt round-robin to the 8 XCDs: group g's rows go to XCD g mod 8
-  const int64_t row = kCodes ? (int64_t)blockIdx.x
+  const int64_t row = LANES ? (int64_t)blockIdx.x * (blockDim.x / LANES) + threadIdx.x / LANES
+                    : kCodes ? (int64_t)blockIdx.x
                              : (int64_t)(blockIdx.x / 128) * 128 + blockIdx.x % 8 * 16 + blockIdx.x / 8 % 16;
   if (row >= a.M) return;
+  auto row_sum = [&](double v) __attribute__((always_inline)) {
+    if constexpr (LANES > 0) return lanes_sum<LANES>(v);
+    else return block_sum(v, lds_sum);
+  };
+  auto row_max = [&](uint32_t v) __attribute__((always_inline)) {
+    if constexpr (LANES > 0) return lanes_max<LANES>(v);
+    else return block_max(v, lds_max);
+  };
   const uint8_t* const x = a.x + row * a.x_stride * 2;
   const uint8_t* const r = a.residual != nullptr ? a.residual + row * a.r_stride * 2 : nullptr;
   uint8_t* const hrow = a.h != nullptr ? a.h + row * K * 2 : nullptr;
@@ -256,14 +286,14 @@ __global__ __launch_bounds__(kWave* kMaxWaves) void rmsnorm_kernel(NormArgs a) {
       u32x4 rv[NV];
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
-        const int k = (i * (int)blockDim.x + tid) * 8;
+        const int k = (i * threads + tid) * 8;
         v[i] = load(x, k);
         rv[i] = r != nullptr ? load(r, k) : none;
         g[i] = a.gain != nullptr ? load(a.gain, k) : none;
       }
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
-        const int k = (i * (int)blockDim.x + tid) * 8;
+        const int k = (i * threads + tid) * 8;
         v[i] = sum_of(settled(v[i], k), settled(rv[i], k));
         g[i] = settled(g[i], k);
       }
@@ -271,15 +301,15 @@ __global__ __launch_bounds__(kWave* kMaxWaves) void rmsnorm_kernel(NormArgs a) {
     double sum = 0.0;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int k = (i * (int)blockDim.x + tid) * 8;
+      const int k = (i * threads + tid) * 8;
       if (hrow != nullptr) store(hrow, k, v[i]);
       sum += squares(v[i]);
     }
-    const float f = factor(block_sum(sum, lds_sum));
+    const float f = factor(row_sum(sum));
     uint32_t m = 0u;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int k = (i * (int)blockDim.x + tid) * 8;
+      const int k = (i * threads + tid) * 8;
       v[i] = cut(normed(v[i], g[i], f), k);
       if (yrow != nullptr) store(yrow, k, v[i]);
       if (kCodes) m = fold_magnitude<T>(m, v[i]);
@@ -287,9 +317,9 @@ __global__ __launch_bounds__(kWave* kMaxWaves) void rmsnorm_kernel(NormArgs a) {
     }
     if constexpr (kCodes) {
       CodeScale cs;
-      cs.set<T>(block_max(widest<T>(m), lds_max), a.q);
+      cs.set<T>(row_max(widest<T>(m)), a.q);
 #pragma unroll
-      for (int i = 0; i < NV; ++i) store_codes((i * (int)blockDim.x + tid) * 8, v[i], cs);
+      for (int i = 0; i < NV; ++i) store_codes((i * threads + tid) * 8, v[i], cs);
       if (tid == 0) a.scale[row] = (uint16_t)cs.bits;
     }
   } else {
@@ -298,12 +328,12 @@ __global__ __launch_bounds__(kWave* kMaxWaves) void rmsnorm_kernel(NormArgs a) {
       return sum_of(settled(xv, k), settled(rv, k));
     };
     double sum = 0.0;
-    for (int i = tid; i < vectors; i += (int)blockDim.x) {
+    for (int i = tid; i < vectors; i += threads) {
       const u32x4 h = load_h(i * 8);
       if (hrow != nullptr) store(hrow, i * 8, h);
       sum += squares(h);
     }
-    const float f = factor(block_sum(sum, lds_sum));
+    const float f = factor(row_sum(sum));
     // (h may have replaced x or the residual: it is read back, by the thread that wrote it)
     auto load_y = [&](int k) __attribute__((always_inline)) {
       const u32x4 g = a.gain != nullptr ? load(a.gain, k) : none;
@@ -311,7 +341,7 @@ __global__ __launch_bounds__(kWave* kMaxWaves) void rmsnorm_kernel(NormArgs a) {
       return cut(normed(h, settled(g, k), f), k);
     };
     uint32_t m = 0u;
-    for (int i = tid; i < vectors; i += (int)blockDim.x) {
+    for (int i = tid; i < vectors; i += threads) {
       const u32x4 y = load_y(i * 8);
       if (yrow != nullptr) store(yrow, i * 8, y);
       if (kCodes) m = fold_magnitude<T>(m, y);
@@ -319,19 +349,21 @@ __global__ __launch_bounds__(kWave* kMaxWaves) void rmsnorm_kernel(NormArgs a) {
     }
     if constexpr (kCodes) {
       CodeScale cs;
-      cs.set<T>(block_max(widest<T>(m), lds_max), a.q);
-      for (int i = tid; i < vectors; i += (int)blockDim.x) store_codes(i * 8, load_y(i * 8), cs);
+      cs.set<T>(row_max(widest<T>(m)), a.q);
+      for (int i = tid; i < vectors; i += threads) store_codes(i * 8, load_y(i * 8), cs);
       if (tid == 0) a.scale[row] = (uint16_t)cs.bits;
     }
   }
 }
 
 // (2 code + 1) scale, eight elements of a row per thread: bound by memory, 1
-// byte in and 2 or 4 out per element.
+// byte in and 2 or 4 out per element.  A workgroup takes 2^shift threads' worth of
+// 256 >> shift rows: one of `parts` parts of a long row, or several short rows.
 struct CodesArgs {
   const int8_t* codes;
   const uint16_t* scale;
-  int K, parts;
+  int64_t rows;
+  int K, parts, shift;
   uint8_t* out;
 };
 template <class T, bool kStream>
@@ -340,9 +372,9 @@ __global__ __launch_bounds__(256) void dequantize_codes_kernel(CodesArgs a) {
   const uint16_t* const scale = a.scale;
   const int K = a.K, parts = a.parts;
   uint8_t* const out = a.out;
-  const int64_t row = blockIdx.x / (unsigned)parts;
-  const int k = ((int)(blockIdx.x % (unsigned)parts) * 256 + (int)threadIdx.x) * 8;
-  if (k >= K) return;
+  const int64_t row = ((int64_t)(blockIdx.x / (unsigned)parts) << (8 - a.shift)) + (threadIdx.x >> a.shift);
+  const int k = ((int)(blockIdx.x % (unsigned)parts << a.shift) + (int)(threadIdx.x & ((1u << a.shift) - 1u))) * 8;
+  if (row >= a.rows || k >= K) return;
   const float s = Half::to_float(scale[row]);
   const int8_t* const src = codes + row * K + k;
   typedef uint32_t any_u32x2 __attribute__((ext_vector_type(2), aligned(1)));
@@ -378,14 +410,25 @@ hipError_t launch_norm_as(const NormArgs& a, int64_t rows, hipStream_t s) {
   // rows of the launch, by whole groups of 128 for the MX4 mapping
   const unsigned grid = (unsigned)(kCodes ? rows : (rows + 127) / 128 * 128);
   const int vectors = (kCodes ? a.K + 7 : (a.K + kStep - 1) / kStep * kStep) / 8;
+  // Many rows of up to 64 vectors: several to a workgroup, with MX4 a group's 16
+  // (16384 x 128 into codes 12.0 us with a workgroup each, 5.0 so, 2048 x 300 5.7 and
+  // 4.2, 256 x 512 3.0 and 3.3; into MX4 2048 x 300 4.9 and 4.7, 1024 x 512 3.2 and 3.9).
+  if (vectors <= 64 && rows >= (kCodes ? 1024 : 2048)) {
+    const int lanes = kCodes && vectors <= 16 ? 16 : vectors <= 32 ? 32 : 64;
+    const int together = kCodes ? 256 / lanes : kGroup;
+    const dim3 blocks((unsigned)((rows + together - 1) / together)), wide((unsigned)(together * lanes));
+    if (lanes == 64) return launch_kernel(rmsnorm_kernel<T, 1, 64, kCodes, kWhole>, blocks, wide, 0, s, a);
+    if (lanes == 32) return launch_kernel(rmsnorm_kernel<T, 1, 32, kCodes, kWhole>, blocks, wide, 0, s, a);
+    if constexpr (kCodes) return launch_kernel(rmsnorm_kernel<T, 1, 16, kCodes, kWhole>, blocks, wide, 0, s, a);
+  }
   auto threads = [&](int per) { return dim3((unsigned)((vectors + per * kWave - 1) / (per * kWave) * kWave)); };
   // One vector per thread for few rows (a row alone, 1 x 4096: 3.3 us in a graph
   // against 3.6 with two), two where rows queue and a wave's fixed share of the
   // work counts (2048 x 4096 into codes: 14.1 against 14.6), or are long.
-  if (vectors <= 512 && rows < 1024) return launch_kernel(rmsnorm_kernel<T, 1, kCodes, kWhole>, dim3(grid), threads(1), 0, s, a);
-  if (vectors <= 2048) return launch_kernel(rmsnorm_kernel<T, 2, kCodes, kWhole>, dim3(grid), threads(2), 0, s, a);
-  if (vectors <= 4096) return launch_kernel(rmsnorm_kernel<T, 4, kCodes, kWhole>, dim3(grid), threads(4), 0, s, a);
-  return launch_kernel(rmsnorm_kernel<T, 0, kCodes, kWhole>, dim3(grid), dim3(kWave * kMaxWaves), 0, s, a);
+  if (vectors <= 512 && rows < 1024) return launch_kernel(rmsnorm_kernel<T, 1, 0, kCodes, kWhole>, dim3(grid), threads(1), 0, s, a);
+  if (vectors <= 2048) return launch_kernel(rmsnorm_kernel<T, 2, 0, kCodes, kWhole>, dim3(grid), threads(2), 0, s, a);
+  if (vectors <= 4096) return launch_kernel(rmsnorm_kernel<T, 4, 0, kCodes, kWhole>, dim3(grid), threads(4), 0, s, a);
+  return launch_kernel(rmsnorm_kernel<T, 0, 0, kCodes, kWhole>, dim3(grid), dim3(kWave * kMaxWaves), 0, s, a);
 }
 
 template <class T, bool kCodes>
@@ -441,12 +484,14 @@ hipError_t launch_rmsnorm(int M, int K, int type, const void* x, int64_t x_strid
 hipError_t launch_dequantize_codes(const int8_t* codes, const uint16_t* scale, int M, int K, int type, void* out,
                                    hipStream_t s) {
   const int parts = (K + 2047) / 2048;
+  int shift = 0;
+  while (shift < 8 && (8 << shift) < K) ++shift;
   const int64_t most = ((int64_t)1 << 23) / parts > 0 ? ((int64_t)1 << 23) / parts : 1;  // rows of a launch
   const int size = type == APT_TYPE_FP32 ? 4 : 2;
   for (int64_t r0 = 0; r0 < M; r0 += most) {
     const int64_t rows = M - r0 < most ? M - r0 : most;
-    const dim3 grid((unsigned)(rows * parts)), block(256);
-    const CodesArgs a{codes + r0 * K, scale + r0, K, parts, static_cast<uint8_t*>(out) + r0 * K * size};
+    const dim3 grid((unsigned)((((rows - 1) >> (8 - shift)) + 1) * parts)), block(256);
+    const CodesArgs a{codes + r0 * K, scale + r0, rows, K, parts, shift, static_cast<uint8_t*>(out) + r0 * K * size};
     const bool stream = streams(a.out, K, size);
     hipError_t e;
     switch (type) {

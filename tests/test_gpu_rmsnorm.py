@@ -166,3 +166,44 @@ def test_norm_into_the_products(M):
     got = apt.mx4_gemm(op, pw, torch.float32)
     assert torch.equal(got, apt.mx4_gemm_act(y16, pw, torch.float32))
     check_product(got, ref.values(*ref.quantize(y)), ref.values(*wm), K, "fp32")
+
+
+# several rows to a workgroup: full and ragged workgroups, rows of every width that shares one
+SHORT = [(1, 128), (15, 128), (17, 120), (33, 127), (1000, 128), (1024, 64), (1039, 120), (1100, 8), (1027, 127),
+         (1040, 129), (1500, 200), (1033, 256), (1050, 260), (1029, 500), (2100, 512), (1031, 1),
+         (2051, 250), (2049, 120), (2063, 31), (2048, 256), (2060, 481)]
+
+
+@pytest.mark.parametrize("kind", ["fp16", "bf16"])
+@pytest.mark.parametrize("M,K", SHORT)
+def test_norm_of_short_rows(M, K, kind):
+    x, r, g = inputs(M + K, M, K, kind)
+    h, y = ref.norm(x, r, g, EPS, kind)
+    codes, scale, got_h, got_y = apt.rmsnorm_codes(on(x, kind), on(g, kind), 6, EPS, residual=on(r, kind), out_y=True)
+    want_c, want_s = ref.codes(y, 6)
+    same(got_h, h)
+    same(got_y, y)
+    same(scale, want_s)
+    assert np.array_equal(codes.cpu().numpy(), want_c)
+    op, got_h, got_y = apt.rmsnorm_mx4(on(x, kind), on(g, kind), EPS, residual=on(r, kind), out_y=True)
+    same(got_h, h)
+    same(got_y, y)
+    same_operand(op, *ref.quantize(y))
+
+
+@pytest.mark.parametrize("kind", ["fp16", "bf16", "fp32"])
+@pytest.mark.parametrize("M,K", SHORT + [(7, 1000), (5, 1030), (9, 2048)])
+def test_values_of_short_rows(M, K, kind):
+    g = np.random.default_rng(M + K)
+    codes, scale = g.integers(-128, 128, (M, K)).astype(np.int8), np.exp(g.standard_normal(M)).astype(np.float16)
+    got = apt.dequantize(torch.from_numpy(codes).cuda(), torch.from_numpy(scale).cuda(), TYPES[kind])
+    same(got, ref.rounded((2.0 * codes + 1) * scale.astype(np.float64)[:, None], kind))
+
+
+def test_a_bad_short_row_stays_alone():
+    x = np.ones((1030, 96))
+    x[5, 3], x[20, 95] = np.nan, np.inf
+    codes, scale, _ = apt.rmsnorm_codes(dev(x, "bf16"), None, 8, EPS)
+    bad = np.isnan(f64(scale))
+    assert bad[5] and bad[20] and bad.sum() == 2 and not codes[5].any() and not codes[20].any()
+    assert (codes.cpu().numpy()[~bad] == 127).all()
