@@ -133,38 +133,20 @@ __device__ __forceinline__ uint32_t codes_of(const u32x4* v, float scale) {
   return c;
 }
 
-// One 16-byte vector of a row from element k on.  A vector load at an address
-// that is no multiple of 4 takes several times as long (16 rows of 2816 fp16
-// values into MX4: 4.6 us in a graph from odd elements, 3.0 from even ones), so
-// load_split reads the dwords that hold the vector and shifts them; it reads no
-// dword that holds none of it.
+// One 16-byte vector of a row from element k on, at any address (as fast as an
+// aligned one where neighbouring lanes read neighbouring vectors: 2048 x 4095 and
+// 2048 x 4096 norms within 5%).
 template <class T>
 __device__ __forceinline__ u32x4 load_whole(const uint8_t* row, int k) {
   return *reinterpret_cast<const any_u32x4*>(row + (int64_t)k * T::kBytes);
 }
-typedef uint32_t dword_u32x4 __attribute__((ext_vector_type(4), aligned(4)));
-template <class T>
-__device__ __forceinline__ u32x4 load_split(const uint8_t* row, int k) {
-  if constexpr (T::kBytes == 4) return load_whole<T>(row, k);
-  const uint8_t* const p = row + (int64_t)k * T::kBytes;
-  const uint32_t odd = (uint32_t)reinterpret_cast<uintptr_t>(p) & 2u;
-  const u32x4 v = *reinterpret_cast<const dword_u32x4*>(p - odd);
-  const uint32_t last = *reinterpret_cast<const uint32_t*>(p - odd + (odd ? 16 : 12));
-  const uint32_t s = odd * 8u;
-  return u32x4{__builtin_amdgcn_alignbit(v[1], v[0], s), __builtin_amdgcn_alignbit(v[2], v[1], s),
-               __builtin_amdgcn_alignbit(v[3], v[2], s), __builtin_amdgcn_alignbit(last, v[3], s)};
-}
 // The same near a row's end, in two steps so that several loads leave before the
 // first is waited for: load_near reads the vector, or the row's last whole one
 // where it would cross the end, and settle shifts that one down and leaves zero
-// bits from element K on.  (kSplit: rows may start at any element.  Rows shorter
-// than a vector take element loads.)
-template <class T, bool kSplit>
+// bits from element K on.  (Rows shorter than a vector take element loads.)
+template <class T>
 __device__ __forceinline__ u32x4 load_near(const uint8_t* row, int k, int K) {
-  if (K >= T::kVec) {
-    const int at = min(k, K - T::kVec);
-    return kSplit ? load_split<T>(row, at) : load_whole<T>(row, at);
-  }
+  if (K >= T::kVec) return load_whole<T>(row, min(k, K - T::kVec));
   u32x4 v = {0u, 0u, 0u, 0u};
   if constexpr (T::kBytes == 4) {
     const uint32_t* const p = reinterpret_cast<const uint32_t*>(row);
@@ -235,9 +217,16 @@ __device__ __forceinline__ void store_vector(uint8_t* row, int k, int K, u32x4 v
 // bytes, neighbouring lanes fill whole lines, and keeping an output out of L2
 // leaves it to what is read (norm of 2048 x 8192 into codes 26.6 -> 21.5 us in a
 // graph, MX4 values of 2048 x 4096 5.4 -> 4.6, product 2048 x 11008 x 4096 46.4 ->
-// 45.5); lines that two stores share cost more so (333 x 2999 3.7 -> 4.1).
+// 45.5).  Lines that two stores share cost more so (product 2048 x 11007 x 4096 into
+// fp32 79 -> 94).
 __host__ __device__ __forceinline__ bool streams(const void* base, int64_t K, int bytes) {
   return ((reinterpret_cast<uintptr_t>(base) | (uintptr_t)(K * bytes)) & 15) == 0;
+}
+// The same for values, whose waves write whole rows' runs: large outputs are
+// streamed also where rows share lines (2048 x 11007 bf16 16.8 -> 13.7 us, 512 x 5001
+// 3.65 -> 3.85).
+inline bool streams_values(const void* base, int64_t rows, int64_t K, int bytes) {
+  return streams(base, K, bytes) || rows * K * bytes >= (int64_t)12 << 20;
 }
 
 // Launches (arguments validated by the ABI).

@@ -55,25 +55,17 @@ __global__ __launch_bounds__(kWave* kWaves) void quantize_kernel(Rows a) {
   const uint8_t* const src = x + (real ? row : 0) * stride * T::kBytes;
   const int k0 = (int)(unit % o.steps) * kStep;
   u32x4 v[4][kPieces];
-  const bool dwords = T::kBytes == 4 || ((reinterpret_cast<uintptr_t>(x) | (uintptr_t)(stride * 2)) & 3) == 0;
   auto place = [&](int i, int j) __attribute__((always_inline)) { return k0 + i * 2 * kBlock + lane % 8 * 8 + j * T::kVec; };
-  if (k0 + kStep <= K && dwords) {
+  if (k0 + kStep <= K) {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
       for (int j = 0; j < kPieces; ++j) v[i][j] = load_whole<T>(src, place(i, j));
   } else {
-    if (dwords) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int j = 0; j < kPieces; ++j) v[i][j] = load_near<T, false>(src, place(i, j), K);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < kPieces; ++j) v[i][j] = load_near<T, true>(src, place(i, j), K);
-    }
+      for (int j = 0; j < kPieces; ++j) v[i][j] = load_near<T>(src, place(i, j), K);
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -216,7 +208,7 @@ hipError_t launch_quantize(const void* x, int type, int rows, int K, int64_t str
 
 template <class T>
 static hipError_t launch_dequantize_of(const Operand& o, int rows, int K, void* out, hipStream_t s) {
-  return launch_kernel(streams(out, K, T::kBytes) ? dequantize_kernel<T, true> : dequantize_kernel<T, false>,
+  return launch_kernel(streams_values(out, rows, K, T::kBytes) ? dequantize_kernel<T, true> : dequantize_kernel<T, false>,
                        dim3(unit_blocks(o, kValueParts)), dim3(kWave * kWaves), 0, s, Rows{static_cast<uint8_t*>(out), rows, K, K, o});
 }
 

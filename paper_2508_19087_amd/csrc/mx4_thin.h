@@ -79,8 +79,7 @@ struct RowShare {
   static __device__ __forceinline__ int quotient(int x, int d) {
     return (int)(((float)x + 0.5f) * __builtin_amdgcn_rcpf((float)d));
   }
-  template <bool kSplit>
-  __device__ __forceinline__ void load_as(const ThinParams& p, int i0) {
+  __device__ __forceinline__ void load(const ThinParams& p, int i0) {
     const int per_row = p.steps * (kStep / 8), all = per_row * p.M;
 #pragma unroll
     for (int i = 0; i < kHeld; ++i) {
@@ -88,12 +87,8 @@ struct RowShare {
       const int m = quotient(x, per_row), k = (x - m * per_row) * 8;
       const uint8_t* const row = p.x + m * p.x_stride * X::kBytes;
 #pragma unroll
-      for (int j = 0; j < kPieces; ++j) v[i][j] = load_near<X, kSplit>(row, k + j * X::kVec, p.K);
+      for (int j = 0; j < kPieces; ++j) v[i][j] = load_near<X>(row, k + j * X::kVec, p.K);
     }
-  }
-  __device__ __forceinline__ void load(const ThinParams& p, int i0) {
-    if (X::kBytes == 4 || ((reinterpret_cast<uintptr_t>(p.x) | (uintptr_t)(p.x_stride * 2)) & 3) == 0) load_as<false>(p, i0);
-    else load_as<true>(p, i0);
   }
   __device__ __forceinline__ void store(const ThinParams& p, uint8_t* lds, int i0) {
     const int per_row = p.steps * (kStep / 8), all = per_row * p.M;

@@ -177,7 +177,7 @@ struct CodeScale {
 // is read again in each pass); LANES: 0, or the lanes that a row takes, several
 // rows to a workgroup; kCodes: q-bit codes, else MX4; kWhole: K is a
 // multiple of 8, so that no vector is cut by the row's end, and every row starts
-// at a multiple of 4 bytes where it is read and of 16 where it is written.
+// at a multiple of 16 bytes where it is written.
 template <class T, int NV, int LANES, bool kCodes, bool kWhole>
 __global__ __launch_bounds__(kWave* kMaxWaves) void rmsnorm_kernel(NormArgs a) {
   __shared__ double lds_sum[kMaxWaves];
@@ -210,13 +210,13 @@ __global__ __launch_bounds__(kWave* kMaxWaves) void rmsnorm_kernel(NormArgs a) {
   const u32x4 none = {0u, 0u, 0u, 0u};
   auto load = [&](const uint8_t* p, int k) __attribute__((always_inline)) {
     if constexpr (kWhole) return k < K ? load_whole<T>(p, k) : none;
-    else return load_near<T, true>(p, k, K);
+    else return load_near<T>(p, k, K);
   };
   auto settled = [&](u32x4 v, int k) __attribute__((always_inline)) { return kWhole ? v : settle<T>(v, k, K); };
   // (h goes past the cache where the row stays in registers and is not read back)
   auto store = [&](uint8_t* p, int k, u32x4 v) __attribute__((always_inline)) {
     if (kWhole && k < K) store_bytes<2, (NV > 0)>(p + (int64_t)k * 2, 16, v);
-    if (!kWhole) store_vector<T>(p, k, K, v);
+    if (!kWhole) store_vector<T, (NV > 0)>(p, k, K, v);
   };
   // (0 * an infinite or NaN factor: the elements behind K stay 0)
   auto cut = [&](u32x4 v, int k) __attribute__((always_inline)) {
@@ -433,10 +433,8 @@ hipError_t launch_norm_as(const NormArgs& a, int64_t rows, hipStream_t s) {
 
 template <class T, bool kCodes>
 hipError_t launch_norm_of(const NormArgs& a, int64_t rows, hipStream_t s) {
-  uintptr_t at = reinterpret_cast<uintptr_t>(a.x) | reinterpret_cast<uintptr_t>(a.gain) | (uintptr_t)(a.x_stride * 2);
-  if (a.residual != nullptr) at |= reinterpret_cast<uintptr_t>(a.residual) | (uintptr_t)(a.r_stride * 2);
-  return at % 4 == 0 && streams(a.h, a.K, 2) && streams(a.y, a.K, 2) ? launch_norm_as<T, kCodes, true>(a, rows, s)
-                                                                      : launch_norm_as<T, kCodes, false>(a, rows, s);
+  return streams(a.h, a.K, 2) && streams(a.y, a.K, 2) ? launch_norm_as<T, kCodes, true>(a, rows, s)
+                                                      : launch_norm_as<T, kCodes, false>(a, rows, s);
 }
 
 // A launch holds fewer than 2^32 threads: at 1024 a row, this many rows (whole
@@ -492,7 +490,7 @@ hipError_t launch_dequantize_codes(const int8_t* codes, const uint16_t* scale, i
     const int64_t rows = M - r0 < most ? M - r0 : most;
     const dim3 grid((unsigned)((((rows - 1) >> (8 - shift)) + 1) * parts)), block(256);
     const CodesArgs a{codes + r0 * K, scale + r0, rows, K, parts, shift, static_cast<uint8_t*>(out) + r0 * K * size};
-    const bool stream = streams(a.out, K, size);
+    const bool stream = streams_values(a.out, rows, K, size);
     hipError_t e;
     switch (type) {
       case APT_TYPE_FP16:
