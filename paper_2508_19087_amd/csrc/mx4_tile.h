@@ -76,7 +76,7 @@ __device__ __forceinline__ u32x2 join4(float a, float b, float c, float d) {
 template <class T, int MB, int NB, int WD>
 __global__ __launch_bounds__(kTileWaves* kWave, (MB * NB >= 12 ? 1 : 2)) void tile_kernel(GemmParams p) {
   constexpr int kACodes = MB * 2 * kCodeBytes, kAScales = MB * 2 * kScaleBytes;
-  constexpr int kSlot = 32 * (128 + 16);  // epilogue: 32 rows of 128 bytes, padded
+  constexpr int kSlot = 32 * (128 + 16);  // epilogue: 32 rows of 128 bytes or 16 of 256, padded
   constexpr int kStage = kACodes + kAScales > kSlot ? kACodes + kAScales : kSlot;
   constexpr int kSlots = 4 * MB;  // MFMA groups of a step
   __shared__ __attribute__((aligned(16))) uint8_t stage0[kStage];
@@ -264,42 +264,48 @@ __global__ __launch_bounds__(kTileWaves* kWave, (MB * NB >= 12 ? 1 : 2)) void ti
   if (t + 1 < S) step(stage1, stage2, stage0, 1, t + 1, std::false_type{});
   if (t + 2 < S) step(stage2, stage3, stage1, 2, t + 2, std::false_type{});
 
-  // ---- epilogue: 32 rows at a time through the wave's slot (stage `wave`), so
-  // that stores are whole runs of 64 or 128 bytes of an output row.  The MFMA
+  // ---- epilogue: through the wave's slot (stage `wave`), so that stores are whole
+  // runs of all its columns of an output row (2048 x 11007 x 4096 into fp32, whose
+  // rows share lines: 75 us with runs of 256 bytes, 79 with two of 128).  The MFMA
   // leaves lane (r, h) columns 8 g + 4 h + 0..3 of row r.
   __builtin_amdgcn_s_waitcnt(0x0070);  // the last (unused) loads have landed
   __builtin_amdgcn_s_barrier();
-  constexpr int kStride = 128 + 16;
+  // A pass takes 32 rows of 64 or 128 bytes, or 16 of 256.
+  constexpr int kRowBytes = NB * 32 * T::kBytes, kPassRows = kRowBytes > 128 ? 16 : 32;
+  constexpr int kStride = kRowBytes + 16;
+  static_assert(kPassRows * kStride <= kSlot, "a pass fits its slot");
   uint8_t* const slot = wave == 0 ? stage0 : wave == 1 ? stage1 : wave == 2 ? stage2 : stage3;
   const int nw = n0 * (NB * 128) + wave * (NB * 32);
-  constexpr int kCols = T::kBytes == 4 ? 32 : NB * 32;  // columns of a pass
-  constexpr int kRowPieces = kCols * T::kBytes / 16;    // 16-byte pieces of a row
+  constexpr int kRowPieces = kRowBytes / 16;  // 16-byte pieces of a row
   constexpr int kRowsAtOnce = kWave / kRowPieces;
   auto epilogue = [&](auto kStream) __attribute__((always_inline)) {
+    if (nw >= p.N) return;  // uniform: no output here
 #pragma unroll
     for (int a = 0; a < MB; ++a) {
 #pragma unroll
-      for (int b0 = 0; b0 < NB; b0 += kCols / 32) {
-        if ((int64_t)m0 * (MB * 32) + a * 32 >= p.M || nw + b0 * 32 >= p.N) continue;  // uniform: no output here
+      for (int r0 = 0; r0 < 32; r0 += kPassRows) {
+        if ((int64_t)m0 * (MB * 32) + a * 32 + r0 >= p.M) continue;
+        if (kPassRows == 32 || r / kPassRows * kPassRows == r0) {
 #pragma unroll
-        for (int b = b0; b < b0 + kCols / 32; ++b)
+          for (int b = 0; b < NB; ++b)
 #pragma unroll
-          for (int g = 0; g < 4; ++g) {
-            uint8_t* const at = slot + r * kStride + ((b - b0) * 32 + g * 8 + h * 4) * T::kBytes;
-            const v16f& c = acc[b][a];
-            if constexpr (T::kBytes == 4)
-              *reinterpret_cast<v4f*>(at) = v4f{c[g * 4], c[g * 4 + 1], c[g * 4 + 2], c[g * 4 + 3]};
-            else
-              *reinterpret_cast<u32x2*>(at) = join4<T>(c[g * 4], c[g * 4 + 1], c[g * 4 + 2], c[g * 4 + 3]);
-          }
+            for (int g = 0; g < 4; ++g) {
+              uint8_t* const at = slot + (r - r0) * kStride + (b * 32 + g * 8 + h * 4) * T::kBytes;
+              const v16f& c = acc[b][a];
+              if constexpr (T::kBytes == 4)
+                *reinterpret_cast<v4f*>(at) = v4f{c[g * 4], c[g * 4 + 1], c[g * 4 + 2], c[g * 4 + 3]};
+              else
+                *reinterpret_cast<u32x2*>(at) = join4<T>(c[g * 4], c[g * 4 + 1], c[g * 4 + 2], c[g * 4 + 3]);
+            }
+        }
         __builtin_amdgcn_s_waitcnt(0xc07f);  // this wave's LDS writes are done
         __builtin_amdgcn_wave_barrier();
 #pragma unroll
-        for (int j = 0; j < 32 / kRowsAtOnce; ++j) {
+        for (int j = 0; j < kPassRows / kRowsAtOnce; ++j) {
           const int row = j * kRowsAtOnce + lane / kRowPieces, piece = lane % kRowPieces;
           const u32x4 v = *reinterpret_cast<const u32x4*>(slot + row * kStride + piece * 16);
-          const int64_t m = (int64_t)m0 * (MB * 32) + a * 32 + row;
-          const int n = nw + b0 * 32 + piece * T::kVec;
+          const int64_t m = (int64_t)m0 * (MB * 32) + a * 32 + r0 + row;
+          const int n = nw + piece * T::kVec;
           if (m < p.M) store_vector<T, kStream.value>(p.c + m * p.N * T::kBytes, n, p.N, v);
         }
         __builtin_amdgcn_s_waitcnt(0xc07f);  // reads done before the slot is rewritten
