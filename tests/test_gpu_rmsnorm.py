@@ -207,3 +207,24 @@ def test_a_bad_short_row_stays_alone():
     bad = np.isnan(f64(scale))
     assert bad[5] and bad[20] and bad.sum() == 2 and not codes[5].any() and not codes[20].any()
     assert (codes.cpu().numpy()[~bad] == 127).all()
+
+
+@pytest.mark.parametrize("K", [61, 128, 300])
+@pytest.mark.parametrize("which", ["x", "residual"])
+def test_short_rows_in_place(which, K):
+    M = 2100
+    x, r, g = inputs(K, M, K, "bf16")
+    h, y = ref.norm(x, r, g, EPS, "bf16")
+    want_c, want_s = ref.codes(y, 8)
+    for to in ("codes", "mx4"):
+        tx, tr, tg = dev(x, "bf16"), dev(r, "bf16"), dev(g, "bf16")
+        own = tx if which == "x" else tr
+        if to == "codes":
+            codes, scale, got_h = apt.rmsnorm_codes(tx, tg, 8, EPS, residual=tr, h=own)
+            same(scale, want_s)
+            assert np.array_equal(codes.cpu().numpy(), want_c)
+        else:
+            op, got_h = apt.rmsnorm_mx4(tx, tg, EPS, residual=tr, h=own)
+            same_operand(op, *ref.quantize(y))
+        assert got_h is own
+        same(own, h)
