@@ -14,9 +14,9 @@ using namespace mx4;
 // A tile shape and what a step of 256 elements of K costs a workgroup of it, in
 // us: with few compute units busy, with each running one (in between in
 // proportion: what they share, clock, caches and memory, counts long before the
-// chip is full), and its share where each runs several.  `fixed`: what it needs
-// besides more than the others.  Measured at bf16 output on 64 to 2048 rows by
-// 4096 and 11008 columns, K = 4096 to 11008.
+// chip is full), and its share where each runs several.  A launch with its first
+// loads and its outputs takes kTileEnds besides, and `fixed` more.  Measured at
+// bf16 output on 64 to 2048 rows by 4096 to 28672 columns, K = 4096 to 11008.
 struct Tile {
   int mb, nb;
   double few, one, share, fixed;
@@ -29,6 +29,7 @@ constexpr Tile kTiles[] = {
     {8, 2, 0.85, 1.60, 1.60, 4.0},  // 256 x 256, one workgroup per compute unit: its epilogue stands alone
 };
 constexpr int kNumTiles = sizeof(kTiles) / sizeof(kTiles[0]);
+constexpr double kTileEnds = 1.9;
 constexpr double kUnits = 256.0;  // compute units
 
 // Activations given as rows are quantized by the few-row kernel's workgroups
@@ -103,7 +104,7 @@ int kernel_of(int M, int N, int K) {
   if (M <= 32) return best;
   for (int i = 0; i < kNumTiles; ++i) {
     const Tile& t = kTiles[i];
-    consider(kNumThins + i, 1.9 + steps(K) * per_step((double)tiles_of(M, N, t), t) + t.fixed);
+    consider(kNumThins + i, kTileEnds + steps(K) * per_step((double)tiles_of(M, N, t), t) + t.fixed);
   }
   return best;
 }
