@@ -111,7 +111,7 @@ def apt_dequantize_codes(codes, scale, M, K, type, out, stream) -> int:
 # A small call's time is the host's (a launch 3.3 us, each allocation 1.2 to 1.7),
 # so these keep to what a call needs: the C functions are called without the
 # wrappers above, new tensors are made like given ones, and devices are compared
-# by index.
+# by number.
 
 _types = None
 
@@ -135,24 +135,23 @@ def _refuse(where, what):
 _raw_stream = _device = None  # torch's, once it is there
 
 
-def _call(name, device, stream, *args):
-    """The C function `name` of the arguments and the raw stream, on `device`."""
+def _call(name, index, stream, *args):
+    """The C function `name` of the arguments and the raw stream, on the device of number `index`."""
     global _raw_stream, _device
     if _device is None:
         C = _torch()._C
         _raw_stream, _device = C._cuda_getCurrentRawStream, C._cuda_getDevice
-    index = device.index
     if stream is None:
         raw = _raw_stream(index)
     else:
-        if stream.device != device:
+        if stream.device_index != index:
             _refuse(name, "a stream of another device")
         raw = stream.cuda_stream
     f = getattr(_lib or lib(), name)
     if _device() == index:
         status = f(*args, raw)
     else:
-        with _torch().cuda.device(device):
+        with _torch().cuda.device(index):
             status = f(*args, raw)
     if status:
         check(status, name)
@@ -195,28 +194,36 @@ class Mx4:
     data: "object"
     rows: int
     K: int
-    _checked = None  # the data that _data_of has seen
+
+
+def _bytes(rows, K):
+    """apt_mx4_bytes (a call into C takes longer)."""
+    return (rows + 15 >> 4) * (K + 255 >> 8) * 2176 if rows >= 1 and K >= 1 else 0
+
+
+_uint8 = None  # torch's, once it is there
 
 
 def _data_of(a, where):
-    """The data of an operand, checked the first time."""
-    d = a.data
-    if a._checked is not d:
-        n = (_lib or lib()).apt_mx4_bytes(a.rows, a.K)
-        if not (n and d.is_cuda and d.dtype is _torch().uint8 and d.is_contiguous() and d.numel() >= n):
-            _refuse(where, "an operand of %d rows of %d values is %d bytes (uint8) on the device" % (a.rows, a.K, n))
-        a._checked = d
-    return d
+    """The data of an operand and the number of its device, checked at each use: its sizes and its
+    tensor may have changed since the last."""
+    global _uint8
+    if _uint8 is None:
+        _uint8 = _torch().uint8
+    d, rows, K = a.data, a.rows, a.K
+    index = d.get_device()  # (below 0 in host memory)
+    if not (index >= 0 and rows >= 1 and K >= 1 and d.dtype is _uint8 and d.is_contiguous() and
+            d.numel() >= (rows + 15 >> 4) * (K + 255 >> 8) * 2176):
+        _refuse(where, "an operand of %d rows of %d values is %d bytes (uint8) on the device" % (rows, K, _bytes(rows, K)))
+    return d, index
 
 
 def _new_mx4(rows, K, like, stream, where) -> Mx4:
     """An operand on the device of `like`."""
-    n = (_lib or lib()).apt_mx4_bytes(rows, K)
+    n = _bytes(rows, K)
     if n == 0:
         _refuse(where, "%d rows of %d values" % (rows, K))
-    a = Mx4(_new(like, n, _torch().uint8, stream), rows, K)
-    a._checked = a.data
-    return a
+    return Mx4(_new(like, n, _torch().uint8, stream), rows, K)
 
 
 def mx4_quantize(x, stream=None) -> Mx4:
@@ -225,7 +232,7 @@ def mx4_quantize(x, stream=None) -> Mx4:
     M, K = x.shape
     t = _type(x.dtype, "mx4_quantize")
     out = _new_mx4(M, K, x, stream, "mx4_quantize")
-    _call("apt_mx4_quantize", x.device, stream, x.data_ptr(), t, M, K, stride, out.data.data_ptr())
+    _call("apt_mx4_quantize", x.get_device(), stream, x.data_ptr(), t, M, K, stride, out.data.data_ptr())
     return out
 
 
@@ -233,9 +240,9 @@ def mx4_dequantize(a: Mx4, dtype=None, stream=None):
     """The values of an MX4 operand, [rows][K] of `dtype` (by default bf16, which holds all that quantizing gives)."""
     dtype = _torch().bfloat16 if dtype is None else dtype
     t = _type(dtype, "mx4_dequantize")
-    data = _data_of(a, "mx4_dequantize")
+    data, index = _data_of(a, "mx4_dequantize")
     out = _new(data, (a.rows, a.K), dtype, stream)
-    _call("apt_mx4_dequantize", data.device, stream, data.data_ptr(), a.rows, a.K, t, out.data_ptr())
+    _call("apt_mx4_dequantize", index, stream, data.data_ptr(), a.rows, a.K, t, out.data_ptr())
     return out
 
 
@@ -251,16 +258,16 @@ def mx4_pack(codes, scales, K: int, stream=None) -> Mx4:
     out = _new_mx4(rows, K, codes, stream, "mx4_pack")
     with _on_stream(stream):
         codes, scales = codes.contiguous(), scales.contiguous()
-    _call("apt_mx4_pack", codes.device, stream, codes.data_ptr(), scales.data_ptr(), rows, K, out.data.data_ptr())
+    _call("apt_mx4_pack", codes.get_device(), stream, codes.data_ptr(), scales.data_ptr(), rows, K, out.data.data_ptr())
     return out
 
 
 def mx4_unpack(a: Mx4, stream=None):
     """(codes, scales) of an MX4 operand as mx4_pack takes them."""
-    data = _data_of(a, "mx4_unpack")
+    data, index = _data_of(a, "mx4_unpack")
     codes = _new(data, (a.rows, -(-a.K // 2)), data.dtype, stream)
     scales = _new(data, (a.rows, -(-a.K // 32)), data.dtype, stream)
-    _call("apt_mx4_unpack", data.device, stream, data.data_ptr(), a.rows, a.K, codes.data_ptr(), scales.data_ptr())
+    _call("apt_mx4_unpack", index, stream, data.data_ptr(), a.rows, a.K, codes.data_ptr(), scales.data_ptr())
     return codes, scales
 
 
@@ -268,12 +275,13 @@ def mx4_gemm(a: Mx4, w: Mx4, dtype=None, stream=None):
     """C = A W^T of two MX4 operands, [a.rows][w.rows] of `dtype` (fp16 by default)."""
     dtype = _torch().float16 if dtype is None else dtype
     t = _type(dtype, "mx4_gemm")
-    ad, wd = _data_of(a, "mx4_gemm"), _data_of(w, "mx4_gemm")
-    device, M, N, K = ad.device, a.rows, w.rows, a.K
-    if K != w.K or wd.device != device:
-        _refuse("mx4_gemm", "operands of %d and %d values a row on %s and %s" % (K, w.K, device, wd.device))
+    ad, index = _data_of(a, "mx4_gemm")
+    wd, at = _data_of(w, "mx4_gemm")
+    M, N, K = a.rows, w.rows, a.K
+    if K != w.K or at != index:
+        _refuse("mx4_gemm", "operands of %d and %d values a row on %s and %s" % (K, w.K, ad.device, wd.device))
     c = _new(ad, (M, N), dtype, stream)
-    _call("apt_mx4_gemm", device, stream, M, N, K, ad.data_ptr(), wd.data_ptr(), t, c.data_ptr())
+    _call("apt_mx4_gemm", index, stream, M, N, K, ad.data_ptr(), wd.data_ptr(), t, c.data_ptr())
     return c
 
 
@@ -285,20 +293,21 @@ def mx4_gemm_act(x, w: Mx4, dtype=None, stream=None, workspace=None):
     M, K = x.shape
     dtype = x.dtype if dtype is None else dtype
     tx, t = _type(x.dtype, "mx4_gemm_act"), _type(dtype, "mx4_gemm_act")
-    device, wd = x.device, _data_of(w, "mx4_gemm_act")
-    if K != w.K or wd.device != device:
-        _refuse("mx4_gemm_act", "rows of %d values on %s for weights of %d on %s" % (K, device, w.K, wd.device))
+    index = x.get_device()
+    wd, at = _data_of(w, "mx4_gemm_act")
+    if K != w.K or at != index:
+        _refuse("mx4_gemm_act", "rows of %d values on %s for weights of %d on %s" % (K, x.device, w.K, wd.device))
     N = w.rows
     if workspace is None:
         n = (_lib or lib()).apt_mx4_gemm_act_workspace_bytes(M, N, K)
         if n:
             workspace = _new(wd, n, wd.dtype, stream)
     else:
-        if workspace.device != device or not workspace.is_contiguous():
+        if workspace.get_device() != index or not workspace.is_contiguous():
             _refuse("mx4_gemm_act", "a contiguous workspace on the rows' device is wanted")
         n = workspace.numel() * workspace.element_size()
     c = _new(x, (M, N), dtype, stream)
-    _call("apt_mx4_gemm_act", device, stream, M, N, K, x.data_ptr(), tx, stride, wd.data_ptr(), t, c.data_ptr(),
+    _call("apt_mx4_gemm_act", index, stream, M, N, K, x.data_ptr(), tx, stride, wd.data_ptr(), t, c.data_ptr(),
           None if workspace is None else workspace.data_ptr(), n)
     return c
 
@@ -349,7 +358,7 @@ def rmsnorm_codes(x, gain, q: int, eps: float, residual=None, h=None, out_y: boo
     y = _new_like(x, x.dtype, stream) if out_y else None
     codes = _new_like(x, torch.int8, stream)
     scale = _new(x, args[0], torch.float16, stream)
-    _call("apt_rmsnorm_codes", x.device, stream, *args, eps, q, None if h is None else h.data_ptr(),
+    _call("apt_rmsnorm_codes", x.get_device(), stream, *args, eps, q, None if h is None else h.data_ptr(),
           None if y is None else y.data_ptr(), codes.data_ptr(), scale.data_ptr())
     return (codes, scale, h, y) if out_y else (codes, scale, h)
 
@@ -360,7 +369,7 @@ def rmsnorm_mx4(x, gain, eps: float, residual=None, h=None, out_y: bool = False,
     x, residual, gain, h, args = _norm_inputs(x, gain, residual, h, stream, "rmsnorm_mx4")
     y = _new_like(x, x.dtype, stream) if out_y else None
     out = _new_mx4(args[0], args[1], x, stream, "rmsnorm_mx4")
-    _call("apt_rmsnorm_mx4", x.device, stream, *args, eps, None if h is None else h.data_ptr(),
+    _call("apt_rmsnorm_mx4", x.get_device(), stream, *args, eps, None if h is None else h.data_ptr(),
           None if y is None else y.data_ptr(), out.data.data_ptr())
     return (out, h, y) if out_y else (out, h)
 
@@ -378,5 +387,5 @@ def dequantize(codes, scale, dtype=None, stream=None):
             codes, scale = codes.contiguous(), scale.contiguous()
     M, K = codes.shape
     out = _new_like(codes, dtype, stream)
-    _call("apt_dequantize_codes", codes.device, stream, codes.data_ptr(), scale.data_ptr(), M, K, t, out.data_ptr())
+    _call("apt_dequantize_codes", codes.get_device(), stream, codes.data_ptr(), scale.data_ptr(), M, K, t, out.data_ptr())
     return out
