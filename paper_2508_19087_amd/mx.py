@@ -59,50 +59,82 @@ def mx_header_functions() -> list:
 
 
 # ---- C entry points, same names -------------------------------------------------
+#
+# (ctypes passes an int modulo 2^32: 2^32 + 16 rows would be 16)
+
+_MOST = 2 ** 31 - 1  # that an int of C holds
+
+
+def _ints(*numbers):
+    """Whether ints of C hold the numbers."""
+    return max(numbers) <= _MOST and min(numbers) >= -_MOST - 1
+
 
 def apt_mx4_bytes(rows, K) -> int:
+    if not _ints(rows, K):
+        return 0
     return int(lib().apt_mx4_bytes(rows, K))
 
 
 def apt_mx4_quantize(x, type, rows, K, stride, mx, stream) -> int:
+    if not _ints(type, rows, K):
+        return APT_ERR_INVALID_ARG
     return lib().apt_mx4_quantize(x, type, rows, K, stride, mx, stream)
 
 
 def apt_mx4_dequantize(mx, rows, K, type, out, stream) -> int:
+    if not _ints(rows, K, type):
+        return APT_ERR_INVALID_ARG
     return lib().apt_mx4_dequantize(mx, rows, K, type, out, stream)
 
 
 def apt_mx4_pack(codes, scales, rows, K, mx, stream) -> int:
+    if not _ints(rows, K):
+        return APT_ERR_INVALID_ARG
     return lib().apt_mx4_pack(codes, scales, rows, K, mx, stream)
 
 
 def apt_mx4_unpack(mx, rows, K, codes, scales, stream) -> int:
+    if not _ints(rows, K):
+        return APT_ERR_INVALID_ARG
     return lib().apt_mx4_unpack(mx, rows, K, codes, scales, stream)
 
 
 def apt_mx4_gemm(M, N, K, a_mx, w_mx, type, c, stream) -> int:
+    if not _ints(M, N, K, type):
+        return APT_ERR_INVALID_ARG
     return lib().apt_mx4_gemm(M, N, K, a_mx, w_mx, type, c, stream)
 
 
 def apt_mx4_gemm_act_workspace_bytes(M, N, K) -> int:
+    if not _ints(M, N, K):
+        return 0
     return int(lib().apt_mx4_gemm_act_workspace_bytes(M, N, K))
 
 
 def apt_mx4_gemm_act(M, N, K, x, x_type, x_stride, w_mx, type, c, workspace, workspace_bytes, stream) -> int:
+    if not _ints(M, N, K, x_type, type):
+        return APT_ERR_INVALID_ARG
     return lib().apt_mx4_gemm_act(M, N, K, x, x_type, x_stride, w_mx, type, c, workspace, workspace_bytes, stream)
 
 
 def apt_rmsnorm_codes(M, K, type, x, x_stride, residual, residual_stride, gain, eps, q, h, y, codes, scale,
                       stream) -> int:
+    if not _ints(M, K, type, q):
+        return APT_ERR_INVALID_ARG
     return lib().apt_rmsnorm_codes(M, K, type, x, x_stride, residual, residual_stride, gain, eps, q, h, y, codes,
                                    scale, stream)
 
 
 def apt_rmsnorm_mx4(M, K, type, x, x_stride, residual, residual_stride, gain, eps, h, y, mx, stream) -> int:
+    if not _ints(M, K, type):
+        return APT_ERR_INVALID_ARG
     return lib().apt_rmsnorm_mx4(M, K, type, x, x_stride, residual, residual_stride, gain, eps, h, y, mx, stream)
 
 
 def apt_dequantize_codes(codes, scale, M, K, type, out, stream) -> int:
+    if not _ints(M, K, type):
+        return APT_ERR_INVALID_ARG
     return lib().apt_dequantize_codes(codes, scale, M, K, type, out, stream)
 
 
@@ -180,6 +212,8 @@ def _rows(x, where, stream):
     if not x.is_cuda or x.dim() != 2:
         _refuse(where, "a CUDA tensor of two dimensions is wanted")
     M, K = x.shape
+    if M > _MOST or K > _MOST:
+        _refuse(where, "%d rows of %d values" % (M, K))
     if x.is_contiguous():
         return x, K
     if (x.stride(1) == 1 or K == 1) and (x.stride(0) >= K or M == 1):
@@ -212,7 +246,7 @@ def _data_of(a, where):
         _uint8 = _torch().uint8
     d, rows, K = a.data, a.rows, a.K
     index = d.get_device()  # (below 0 in host memory)
-    if not (index >= 0 and rows >= 1 and K >= 1 and d.dtype is _uint8 and d.is_contiguous() and
+    if not (index >= 0 and 0 < rows <= _MOST and 0 < K <= _MOST and d.dtype is _uint8 and d.is_contiguous() and
             d.numel() >= (rows + 15 >> 4) * (K + 255 >> 8) * 2176):
         _refuse(where, "an operand of %d rows of %d values is %d bytes (uint8) on the device" % (rows, K, _bytes(rows, K)))
     return d, index
@@ -255,6 +289,8 @@ def mx4_pack(codes, scales, K: int, stream=None) -> Mx4:
             codes.shape[1] == -(-K // 2)):
         _refuse("mx4_pack", "codes [rows][ceil(K / 2)] and scales [rows][ceil(K / 32)]")
     rows = codes.shape[0]
+    if rows > _MOST or K > _MOST:
+        _refuse("mx4_pack", "%d rows of %d values" % (rows, K))
     out = _new_mx4(rows, K, codes, stream, "mx4_pack")
     with _on_stream(stream):
         codes, scales = codes.contiguous(), scales.contiguous()
@@ -353,6 +389,8 @@ def rmsnorm_codes(x, gain, q: int, eps: float, residual=None, h=None, out_y: boo
     h), and y behind them with out_y: h is x + residual, written to `h` where one is given (x or the
     residual themselves among them), to a new tensor where there is a residual, else None."""
     torch = _torch()
+    if not 1 <= q <= 8:
+        _refuse("rmsnorm_codes", "codes of %s bits" % (q, ))
     # (copies that were made stay alive until the call has been enqueued)
     x, residual, gain, h, args = _norm_inputs(x, gain, residual, h, stream, "rmsnorm_codes")
     y = _new_like(x, x.dtype, stream) if out_y else None
@@ -382,10 +420,12 @@ def dequantize(codes, scale, dtype=None, stream=None):
     if not (codes.is_cuda and codes.dim() == 2 and codes.dtype is torch.int8 and scale.dtype is torch.float16 and
             scale.dim() == 1 and scale.shape[0] == codes.shape[0] and scale.device == codes.device):
         _refuse("dequantize", "int8 codes [M][K] and fp16 scales [M] are wanted")
+    M, K = codes.shape
+    if M > _MOST or K > _MOST:
+        _refuse("dequantize", "%d rows of %d values" % (M, K))
     if not (codes.is_contiguous() and scale.is_contiguous()):
         with _on_stream(stream):
             codes, scale = codes.contiguous(), scale.contiguous()
-    M, K = codes.shape
     out = _new_like(codes, dtype, stream)
     _call("apt_dequantize_codes", codes.get_device(), stream, codes.data_ptr(), scale.data_ptr(), M, K, t, out.data_ptr())
     return out

@@ -128,3 +128,78 @@ def test_a_changed_operand_that_still_fits_is_taken(reached):
 @pytest.mark.parametrize("K", [-1, 0, 1, 255, 256, 257, 11008, 2 ** 30])
 def test_sizes_are_the_librarys(rows, K):
     assert mx._bytes(rows, K) == apt.apt_mx4_bytes(rows, K)
+
+
+# ---- sizes that an int of C does not hold -----------------------------------------
+# (C takes them modulo 2^32: 2^32 + 16 rows as 16)
+
+HUGE = [2 ** 31, 2 ** 32 + 16, 2 ** 40 + 256]
+F16, P = apt.APT_TYPE_FP16, 1 << 20
+# (names and arguments in order; the C function is called with the numbers that are asked for)
+ENTRIES = [
+    ("apt_mx4_quantize", dict(x=P, type=F16, rows=16, K=256, stride=2 ** 41, mx=P, stream=None), ("rows", "K", "type")),
+    ("apt_mx4_dequantize", dict(mx=P, rows=16, K=256, type=F16, out=P, stream=None), ("rows", "K", "type")),
+    ("apt_mx4_pack", dict(codes=P, scales=P, rows=16, K=256, mx=P, stream=None), ("rows", "K")),
+    ("apt_mx4_unpack", dict(mx=P, rows=16, K=256, codes=P, scales=P, stream=None), ("rows", "K")),
+    ("apt_mx4_gemm", dict(M=16, N=16, K=256, a_mx=P, w_mx=P, type=F16, c=P, stream=None), ("M", "N", "K", "type")),
+    ("apt_mx4_gemm_act", dict(M=16, N=16, K=256, x=P, x_type=F16, x_stride=2 ** 41, w_mx=P, type=F16, c=P,
+                              workspace=P, workspace_bytes=1 << 40, stream=None), ("M", "N", "K", "type", "x_type")),
+    ("apt_rmsnorm_codes", dict(M=16, K=256, type=F16, x=P, x_stride=2 ** 41, residual=None, residual_stride=0, gain=None,
+                               eps=1e-5, q=8, h=None, y=None, codes=P, scale=P, stream=None), ("M", "K", "type", "q")),
+    ("apt_rmsnorm_mx4", dict(M=16, K=256, type=F16, x=P, x_stride=2 ** 41, residual=None, residual_stride=0, gain=None,
+                             eps=1e-5, h=None, y=None, mx=P, stream=None), ("M", "K", "type")),
+    ("apt_dequantize_codes", dict(codes=P, scale=P, M=16, K=256, type=F16, out=P, stream=None), ("M", "K", "type")),
+]
+
+
+class Library:
+    """A library whose functions record that they were called, and do nothing."""
+
+    def __init__(self):
+        self.calls = []
+
+    def __getattr__(self, name):
+        return lambda *a: self.calls.append(name) or 0
+
+
+@pytest.mark.parametrize("name,args,numbers", ENTRIES, ids=[e[0] for e in ENTRIES])
+def test_entry_points_refuse_numbers_beyond_c(monkeypatch, name, args, numbers):
+    library = Library()
+    monkeypatch.setattr(mx, "_lib", library)
+    assert getattr(apt, name)(**args) == apt.APT_OK and library.calls == [name]
+    for number in numbers:
+        for huge in HUGE + [-2 ** 31 - 1, 2 ** 32 + args[number]]:
+            assert getattr(apt, name)(**(args | {number: huge})) == BAD, (number, huge)
+    assert library.calls == [name]
+
+
+def test_sizes_in_bytes_beyond_c():
+    for huge in HUGE + [-2 ** 32 + 16]:
+        assert apt.apt_mx4_bytes(huge, 1) == 0 and apt.apt_mx4_bytes(1, huge) == 0
+        for sizes in ((huge, 16, 256), (300, huge, 256), (300, 16, huge)):
+            assert apt.apt_mx4_gemm_act_workspace_bytes(*sizes) == 0
+
+
+@pytest.mark.parametrize("huge", HUGE)
+def test_helpers_refuse_sizes_beyond_c(reached, huge):
+    w = operand(16, 256)
+    for shape in ((huge, 256), (16, huge)):
+        x, codes = OnDevice(shape, torch.float16), OnDevice(shape, torch.int8)
+        refused(lambda: apt.mx4_quantize(x))
+        refused(lambda: apt.rmsnorm_codes(x, None, 8, 1e-5))
+        refused(lambda: apt.rmsnorm_mx4(x, None, 1e-5))
+        refused(lambda: apt.dequantize(codes, OnDevice(shape[:1], torch.float16)))
+        refused(lambda: apt.mx4_gemm_act(x, apt.Mx4(w.data, 16, shape[1])))
+        refused(lambda: apt.mx4_pack(OnDevice((shape[0], -(-shape[1] // 2))), OnDevice((shape[0], -(-shape[1] // 32))),
+                                     shape[1]))
+        big = apt.Mx4(OnDevice((2 ** 60, )), *shape)
+        for use in uses(apt.Mx4(big.data, huge, 256)) + [lambda: apt.mx4_dequantize(big), lambda: apt.mx4_unpack(big),
+                                                          lambda: apt.mx4_gemm(big, big)]:
+            refused(use)
+    assert not reached
+
+
+@pytest.mark.parametrize("q", [0, 9, -1, 2 ** 32 + 8])
+def test_norm_refuses_bits_out_of_range(reached, q):
+    refused(lambda: apt.rmsnorm_codes(OnDevice((16, 256), torch.float16), None, q, 1e-5))
+    assert not reached
