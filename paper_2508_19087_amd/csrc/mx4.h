@@ -16,7 +16,7 @@ constexpr int kCodeBytes = kGroup * kStep / 2;        // codes of a group and st
 constexpr int kScaleBytes = kGroup * kStep / kBlock;  // scale bytes of a group and step
 
 inline int64_t groups(int rows) { return ((int64_t)rows + kGroup - 1) / kGroup; }
-inline int steps(int K) { return (K + kStep - 1) / kStep; }
+inline int steps(int K) { return K / kStep + (K % kStep != 0); }  // (any int: sizes are asked for before they are checked)
 inline size_t code_bytes(int rows, int K) { return (size_t)groups(rows) * steps(K) * kCodeBytes; }
 inline size_t operand_bytes(int rows, int K) {
   return (size_t)groups(rows) * steps(K) * (kCodeBytes + kScaleBytes);

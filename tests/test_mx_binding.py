@@ -203,3 +203,9 @@ def test_helpers_refuse_sizes_beyond_c(reached, huge):
 def test_norm_refuses_bits_out_of_range(reached, q):
     refused(lambda: apt.rmsnorm_codes(OnDevice((16, 256), torch.float16), None, q, 1e-5))
     assert not reached
+
+
+@pytest.mark.parametrize("K", [2 ** 31 - 1, 2 ** 31 - 255, 2 ** 31 - 256, 2 ** 30 + 1])
+def test_bytes_of_the_longest_rows(K):
+    for rows in (1, 17, 2 ** 31 - 1):
+        assert apt.apt_mx4_bytes(rows, K) == -(-rows // 16) * -(-K // 256) * 2176
