@@ -94,6 +94,16 @@ apt_status_t apt_mx4_unpack(const void* mx, int rows, int K, uint8_t* codes, uin
 apt_status_t apt_mx4_gemm(int M, int N, int K, const void* a_mx, const void* w_mx, int type, void* c,
                           void* stream);
 
+/* The kernel that apt_mx4_gemm takes for a problem, by the block of outputs that
+ * one of its workgroups makes: 16 x 16, 32 x 16, 32 x 32 or 64 x 32 (the few-row
+ * kernel), or 32 x 128, 64 x 128, 128 x 128, 128 x 256 or 256 x 256 (tiles).  It
+ * depends on the sizes alone.  (apt_mx4_gemm_act without a workspace is the few-row
+ * kernel in blocks of 16 x 16 as well.)
+ *   rows, columns  host, receive the block
+ * Errors: APT_ERR_INVALID_ARG for sizes < 1 or NULL pointers; APT_ERR_UNSUPPORTED
+ * as apt_mx4_gemm. */
+apt_status_t apt_mx4_select(int M, int N, int K, int* rows, int* columns);
+
 /* C = A * W^T with the activations given unpacked and quantized inside the call
  * as apt_mx4_quantize does; the result equals that of apt_mx4_quantize followed
  * by apt_mx4_gemm, bit for bit.  Up to 16 rows of together 16384 elements (rows

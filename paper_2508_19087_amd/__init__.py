@@ -20,6 +20,6 @@ from .apt import (APT_ACT_CODES, APT_ACT_FP16, APT_DECODE_MAX_M, APT_ERR_HIP, AP
                   status_string)
 from .mx import (APT_TYPE_BF16, APT_TYPE_FP16, APT_TYPE_FP32, Mx4, apt_dequantize_codes, apt_mx4_bytes,  # noqa: F401
                  apt_mx4_dequantize, apt_mx4_gemm, apt_mx4_gemm_act, apt_mx4_gemm_act_workspace_bytes,
-                 apt_mx4_pack, apt_mx4_quantize, apt_mx4_unpack, apt_rmsnorm_codes,
+                 apt_mx4_pack, apt_mx4_quantize, apt_mx4_select, apt_mx4_unpack, apt_rmsnorm_codes,
                  apt_rmsnorm_mx4, dequantize, mx4_dequantize, mx4_gemm, mx4_gemm_act, mx4_pack, mx4_quantize,
                  mx4_unpack, mx_header_functions, rmsnorm_codes, rmsnorm_mx4)

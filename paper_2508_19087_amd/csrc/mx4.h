@@ -241,8 +241,9 @@ hipError_t launch_rmsnorm(int M, int K, int type, const void* x, int64_t x_strid
 hipError_t launch_dequantize_codes(const int8_t* codes, const uint16_t* scale, int M, int K, int type, void* out,
                                    hipStream_t s);
 // The product of two operands (mx4_gemm.hip); gemm_tiles: the workgroups of the
-// launch, for the ABI's bound.
+// launch, for the ABI's bound; gemm_block: the outputs that each makes.
 int64_t gemm_tiles(int M, int N, int K);
+void gemm_block(int M, int N, int K, int* rows, int* columns);
 hipError_t launch_gemm(int M, int N, int K, const Operand& a, const Operand& w, int type, void* c, hipStream_t s);
 // The same from rows, quantized in the product's kernel, where gemm_takes_rows.
 bool gemm_takes_rows(int M, int K);

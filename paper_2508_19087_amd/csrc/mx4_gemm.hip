@@ -156,6 +156,12 @@ int64_t gemm_tiles(int M, int N, int K) {
   return k < kNumThins ? blocks_of(M, N, kThins[k]) : tiles_of(M, N, kTiles[k - kNumThins]);
 }
 
+void gemm_block(int M, int N, int K, int* rows, int* columns) {
+  const int k = kernel_of(M, N, K);
+  *rows = k < kNumThins ? 16 * kThins[k].mt : 32 * kTiles[k - kNumThins].mb;
+  *columns = k < kNumThins ? 16 * kThins[k].nt : 128 * kTiles[k - kNumThins].nb;
+}
+
 hipError_t launch_gemm(int M, int N, int K, const Operand& a, const Operand& w, int type, void* c, hipStream_t s) {
   const int k = kernel_of(M, N, K);
   if (k < kNumThins)

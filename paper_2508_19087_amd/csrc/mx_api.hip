@@ -110,6 +110,13 @@ apt_status_t apt_mx4_gemm(int M, int N, int K, const void* a_mx, const void* w_m
                                           static_cast<hipStream_t>(stream)));
 }
 
+apt_status_t apt_mx4_select(int M, int N, int K, int* rows, int* columns) {
+  if (M < 1 || N < 1 || K < 1 || rows == nullptr || columns == nullptr) return APT_ERR_INVALID_ARG;
+  if (!sizes_ok(M, N, K)) return APT_ERR_UNSUPPORTED;
+  apt::mx4::gemm_block(M, N, K, rows, columns);
+  return APT_OK;
+}
+
 size_t apt_mx4_gemm_act_workspace_bytes(int M, int N, int K) {
   if (!sizes_ok(M, N, K) || apt::mx4::gemm_takes_rows(M, K)) return 0;
   return apt::mx4::operand_bytes(M, K);

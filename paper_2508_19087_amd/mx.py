@@ -31,6 +31,7 @@ _SIGNATURES = {
     "apt_mx4_pack": (_int, [_vp, _vp, _int, _int, _vp, _vp]),
     "apt_mx4_unpack": (_int, [_vp, _int, _int, _vp, _vp, _vp]),
     "apt_mx4_gemm": (_int, [_int, _int, _int, _vp, _vp, _int, _vp, _vp]),
+    "apt_mx4_select": (_int, [_int, _int, _int, ctypes.POINTER(_int), ctypes.POINTER(_int)]),
     "apt_mx4_gemm_act_workspace_bytes": (_size, [_int, _int, _int]),
     "apt_mx4_gemm_act": (_int, [_int, _int, _int, _vp, _int, _i64, _vp, _int, _vp, _vp, _size, _vp]),
     "apt_rmsnorm_codes": (_int, [_int, _int, _int, _vp, _i64, _vp, _i64, _vp, ctypes.c_double, _int, _vp, _vp, _vp,
@@ -104,6 +105,15 @@ def apt_mx4_gemm(M, N, K, a_mx, w_mx, type, c, stream) -> int:
     if not _ints(M, N, K, type):
         return APT_ERR_INVALID_ARG
     return lib().apt_mx4_gemm(M, N, K, a_mx, w_mx, type, c, stream)
+
+
+def apt_mx4_select(M, N, K):
+    """(status, rows, columns)."""
+    if not _ints(M, N, K):
+        return APT_ERR_INVALID_ARG, 0, 0
+    rows, columns = _int(0), _int(0)
+    st = lib().apt_mx4_select(M, N, K, ctypes.byref(rows), ctypes.byref(columns))
+    return st, rows.value, columns.value
 
 
 def apt_mx4_gemm_act_workspace_bytes(M, N, K) -> int:
