@@ -107,8 +107,9 @@ apt_status_t apt_mx4_select(int M, int N, int K, int* rows, int* columns);
 /* C = A * W^T with the activations given unpacked and quantized inside the call
  * as apt_mx4_quantize does; the result equals that of apt_mx4_quantize followed
  * by apt_mx4_gemm, bit for bit.  Up to 16 rows of together 16384 elements (rows
- * padded to 256) are quantized by the product's kernel itself; others go through
- * the workspace.
+ * padded to 256) are quantized by the product's kernel itself, three rows or more
+ * while these elements times N / 16 are at most 2^24; others go through the
+ * workspace.
  *   x, x_type, x_stride  as apt_mx4_quantize, M rows
  *   workspace, workspace_bytes  device scratch of at least
  *               apt_mx4_gemm_act_workspace_bytes(M, N, K) bytes, 16-byte aligned

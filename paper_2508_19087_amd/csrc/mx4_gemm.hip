@@ -33,13 +33,21 @@ constexpr double kTileEnds = 1.9;
 constexpr double kUnits = 256.0;  // compute units
 
 // Activations given as rows are quantized by the few-row kernel's workgroups
-// themselves, each on its own, up to this many elements (rows padded to steps).
+// themselves, each on its own, up to kFusedElements elements (rows padded to steps).
 // The conversion takes 0.8 us per 4096 elements and saves a launch, which is 1.5 us
-// of a graph and 4 us of a call's time on the host.  Fused and not, in a graph: 1 x
-// 11008 x 4096 6.1 and 8.4 us, 2 x 11008 x 4096 6.9 and 8.5, 3 x 11008 x 4096 8.1 and 8.4,
-// 4 x 11008 x 4096 9.2 and 8.5 (called by itself 8.7 and 11.0), 4 x 4096 x 4096 5.4 and 5.2
-// (7.0 and 10.9), 6 x 4096 x 4096 7.2 and 5.4, 16 x 4096 x 1024 5.5 and 5.2 (7.1 and 11.1).
+// of a graph and 4 to 5 us of a call's time on the host.  Fused and not, in a graph
+// and by itself: 1 x 11008 x 4096 6.2 and 8.5, 7.3 and 12.5 us; 3 x 11008 x 4096 7.9 and 8.5, 7.6
+// and 12.5; 4 x 11008 x 4096 8.8 and 8.4, 8.5 and 12.4; 4 x 4096 x 4096 5.4 and 5.2, 7.2 and
+// 12.2; 16 x 4096 x 1024 5.4 and 5.1, 7.2 and 12.4; 6 x 4096 x 4096 7.2 and 5.4 in a graph.
+// Every 16 weight rows repeat it, so with many of them it costs more than a launch
+// either way: from kFusedRows on, it ends at kFusedWork elements times groups (4 x
+// 16384 x 4096 10.7 and 10.0, 10.4 and 12.4; 4 x 24576 x 4096 14.2 and 12.3, 13.9 and 12.6;
+// 4 x 32000 x 4096 17.0 and 14.4, 16.7 and 13.9; 16 x 32000 x 1024 12.9 and 9.4, 12.3 and
+// 12.3).  One or two rows' conversion hides behind the weights at any N (2 x 64000 x
+// 4096 22.8 and 24.8, 22.1 and 23.9; 2 x 64000 x 8192 51.7 and 51.0, 47.5 and 48.2).
 constexpr int64_t kFusedElements = 16384;
+constexpr int kFusedRows = 3;
+constexpr int64_t kFusedWork = (int64_t)1 << 24;
 
 int64_t tiles_of(int M, int N, const Tile& t) {
   return ((int64_t)M + t.mb * 32 - 1) / (t.mb * 32) * (((int64_t)N + t.nb * 128 - 1) / (t.nb * 128));
@@ -174,7 +182,10 @@ hipError_t launch_gemm(int M, int N, int K, const Operand& a, const Operand& w, 
   }
 }
 
-bool gemm_takes_rows(int M, int K) { return M <= 16 && (int64_t)M * steps(K) * kStep <= kFusedElements; }
+bool gemm_takes_rows(int M, int N, int K) {
+  const int64_t elements = (int64_t)M * steps(K) * kStep;
+  return M <= 16 && elements <= kFusedElements && (M < kFusedRows || elements * groups(N) <= kFusedWork);
+}
 
 hipError_t launch_gemm_rows(int M, int N, int K, const void* x, int x_type, int64_t x_stride, const Operand& w, int type,
                             void* c, hipStream_t s) {

@@ -118,7 +118,7 @@ apt_status_t apt_mx4_select(int M, int N, int K, int* rows, int* columns) {
 }
 
 size_t apt_mx4_gemm_act_workspace_bytes(int M, int N, int K) {
-  if (!sizes_ok(M, N, K) || apt::mx4::gemm_takes_rows(M, K)) return 0;
+  if (!sizes_ok(M, N, K) || apt::mx4::gemm_takes_rows(M, N, K)) return 0;
   return apt::mx4::operand_bytes(M, K);
 }
 

@@ -64,6 +64,16 @@ def test_rows_quantized_by_the_product(size):
         check_exact(apt.mx4_gemm_act(wide[:, 3:K + 3], w, torch.float32), want, "%s, rows apart" % kind)
 
 
+@pytest.mark.parametrize("size", [(3, 21840, 4000), (3, 21841, 4000), (16, 16384, 1000), (16, 16385, 1000), (2, 33001, 4000)],
+                         ids=lambda s: "%dx%dx%d" % s)
+def test_few_rows_by_many_weight_rows(size):
+    """On both sides of the limit on repeated conversions."""
+    M, N, K = size
+    (_, va), (w, vw) = scaled(M, M, K, 0), scaled(N + 1, N, K, 0)
+    want = (va @ vw.t().contiguous()).float()
+    check_exact(apt.mx4_gemm_act(va.half(), w, torch.float32), want, size)
+
+
 SOME = [(5, 20, 703), (17, 2052, 208), (17, 4206, 2120), (34, 5672, 4797), (33, 20, 353), (4100, 133, 686),
         (193, 8225, 436), (457, 8194, 473), (1089, 7413, 2770)]
 

@@ -64,3 +64,12 @@ def test_select_limits():
     for s in ((1, 1, 2 ** 24 + 1), (2 ** 31 - 1, 1, 1), (1, 2 ** 31 - 1, 257), (2 ** 27, 2 ** 27, 1)):
         assert apt.apt_mx4_select(*s)[0] == apt.APT_ERR_UNSUPPORTED
     assert apt.lib().apt_mx4_select(1, 1, 1, None, None) == apt.APT_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("M,K,most", [(3, 4096, 21840), (4, 4096, 16384), (16, 1024, 16384), (8, 1024, 32768), (3, 256, 349520)])
+def test_rows_are_quantized_once_where_many_weight_rows_repeat_it(M, K, most):
+    """Up to 2^24 elements times groups of 16 weight rows, from three rows on."""
+    assert apt.apt_mx4_gemm_act_workspace_bytes(M, most, K) == 0
+    assert apt.apt_mx4_gemm_act_workspace_bytes(M, most + 1, K) == apt.apt_mx4_bytes(M, K)
+    for rows in (1, 2):
+        assert apt.apt_mx4_gemm_act_workspace_bytes(rows, 128000, K) == 0
