@@ -218,18 +218,20 @@ def _new_like(x, dtype, stream):
 
 
 def _rows(x, where, stream):
-    """x, or a copy (made on the call's stream), as rows of adjacent elements, and the stride of its rows."""
-    if not x.is_cuda or x.dim() != 2:
+    """x, or a copy (made on the call's stream), as rows of adjacent elements: (rows, the stride from one
+    to the next, their number, their length, the number of their device)."""
+    index = x.get_device()  # (below 0 in host memory)
+    if index < 0 or x.dim() != 2:
         _refuse(where, "a CUDA tensor of two dimensions is wanted")
     M, K = x.shape
     if M > _MOST or K > _MOST:
         _refuse(where, "%d rows of %d values" % (M, K))
     if x.is_contiguous():
-        return x, K
+        return x, K, M, K, index
     if (x.stride(1) == 1 or K == 1) and (x.stride(0) >= K or M == 1):
-        return x, (x.stride(0) if M > 1 else K)
+        return x, (x.stride(0) if M > 1 else K), M, K, index
     with _on_stream(stream):
-        return x.contiguous(), K
+        return x.contiguous(), K, M, K, index
 
 
 @dataclass
@@ -272,11 +274,10 @@ def _new_mx4(rows, K, like, stream, where) -> Mx4:
 
 def mx4_quantize(x, stream=None) -> Mx4:
     """Quantizes rows x [M][K] (fp16, bf16 or fp32, a CUDA tensor) to an MX4 operand."""
-    x, stride = _rows(x, "mx4_quantize", stream)
-    M, K = x.shape
+    x, stride, M, K, index = _rows(x, "mx4_quantize", stream)
     t = _type(x.dtype, "mx4_quantize")
     out = _new_mx4(M, K, x, stream, "mx4_quantize")
-    _call("apt_mx4_quantize", x.get_device(), stream, x.data_ptr(), t, M, K, stride, out.data.data_ptr())
+    _call("apt_mx4_quantize", index, stream, x.data_ptr(), t, M, K, stride, out.data.data_ptr())
     return out
 
 
@@ -335,11 +336,9 @@ def mx4_gemm_act(x, w: Mx4, dtype=None, stream=None, workspace=None):
     """C = A W^T for unpacked activations x [M][K] (fp16, bf16 or fp32), quantized to MX4 inside the
     call; [M][w.rows] of `dtype` (by default x's).  A workspace of apt_mx4_gemm_act_workspace_bytes is
     allocated with torch unless one is passed."""
-    x, stride = _rows(x, "mx4_gemm_act", stream)
-    M, K = x.shape
+    x, stride, M, K, index = _rows(x, "mx4_gemm_act", stream)
     dtype = x.dtype if dtype is None else dtype
     tx, t = _type(x.dtype, "mx4_gemm_act"), _type(dtype, "mx4_gemm_act")
-    index = x.get_device()
     wd, at = _data_of(w, "mx4_gemm_act")
     if K != w.K or at != index:
         _refuse("mx4_gemm_act", "rows of %d values on %s for weights of %d on %s" % (K, x.device, w.K, wd.device))
@@ -360,37 +359,36 @@ def mx4_gemm_act(x, w: Mx4, dtype=None, stream=None, workspace=None):
 
 def _norm_inputs(x, gain, residual, h, stream, where):
     """Checked inputs of a norm: x, the residual, the gain, h (given, or made where there is a residual,
-    or None) and the C arguments up to the gain."""
+    or None), the number of their device and the C arguments up to the gain."""
     torch = _torch()
-    dtype, device = x.dtype, x.device
+    dtype = x.dtype
     t = APT_TYPE_FP16 if dtype is torch.float16 else APT_TYPE_BF16 if dtype is torch.bfloat16 else 0
     if not t:
         _refuse(where, "fp16 or bf16 rows are wanted")
-    x, xs = _rows(x, where, stream)
+    x, xs, M, K, index = _rows(x, where, stream)
     shape = x.shape
-    M, K = shape
     rp, rs, gp = None, 0, None
     if residual is not None:
-        if residual.dtype is not dtype or residual.shape != shape or residual.device != device:
+        if residual.dtype is not dtype or residual.shape != shape or residual.get_device() != index:
             _refuse(where, "a residual like x is wanted")
         if residual.is_contiguous():
             rs = K
         else:
-            residual, rs = _rows(residual, where, stream)
+            residual, rs = _rows(residual, where, stream)[:2]
         rp = residual.data_ptr()
     if gain is not None:
-        if gain.dtype is not dtype or gain.dim() != 1 or gain.numel() != K or gain.device != device:
+        if gain.dtype is not dtype or gain.dim() != 1 or gain.numel() != K or gain.get_device() != index:
             _refuse(where, "a gain of x's width, type and device is wanted")
         if not gain.is_contiguous():
             with _on_stream(stream):
                 gain = gain.contiguous()
         gp = gain.data_ptr()
     if h is not None:
-        if h.dtype is not dtype or h.shape != shape or h.device != device or not h.is_contiguous():
+        if h.dtype is not dtype or h.shape != shape or h.get_device() != index or not h.is_contiguous():
             _refuse(where, "a contiguous h like x is wanted")
     elif residual is not None:
         h = _new_like(x, dtype, stream)
-    return x, residual, gain, h, (M, K, t, x.data_ptr(), xs, rp, rs, gp)
+    return x, residual, gain, h, index, (M, K, t, x.data_ptr(), xs, rp, rs, gp)
 
 
 def rmsnorm_codes(x, gain, q: int, eps: float, residual=None, h=None, out_y: bool = False, stream=None):
@@ -402,11 +400,11 @@ def rmsnorm_codes(x, gain, q: int, eps: float, residual=None, h=None, out_y: boo
     if not 1 <= q <= 8:
         _refuse("rmsnorm_codes", "codes of %s bits" % (q, ))
     # (copies that were made stay alive until the call has been enqueued)
-    x, residual, gain, h, args = _norm_inputs(x, gain, residual, h, stream, "rmsnorm_codes")
+    x, residual, gain, h, index, args = _norm_inputs(x, gain, residual, h, stream, "rmsnorm_codes")
     y = _new_like(x, x.dtype, stream) if out_y else None
     codes = _new_like(x, torch.int8, stream)
     scale = _new(x, args[0], torch.float16, stream)
-    _call("apt_rmsnorm_codes", x.get_device(), stream, *args, eps, q, None if h is None else h.data_ptr(),
+    _call("apt_rmsnorm_codes", index, stream, *args, eps, q, None if h is None else h.data_ptr(),
           None if y is None else y.data_ptr(), codes.data_ptr(), scale.data_ptr())
     return (codes, scale, h, y) if out_y else (codes, scale, h)
 
@@ -414,10 +412,10 @@ def rmsnorm_codes(x, gain, q: int, eps: float, residual=None, h=None, out_y: boo
 def rmsnorm_mx4(x, gain, eps: float, residual=None, h=None, out_y: bool = False, stream=None):
     """As rmsnorm_codes with the row quantized to MX4.  Returns (Mx4, h), and y behind them with out_y."""
     # (copies that were made stay alive until the call has been enqueued)
-    x, residual, gain, h, args = _norm_inputs(x, gain, residual, h, stream, "rmsnorm_mx4")
+    x, residual, gain, h, index, args = _norm_inputs(x, gain, residual, h, stream, "rmsnorm_mx4")
     y = _new_like(x, x.dtype, stream) if out_y else None
     out = _new_mx4(args[0], args[1], x, stream, "rmsnorm_mx4")
-    _call("apt_rmsnorm_mx4", x.get_device(), stream, *args, eps, None if h is None else h.data_ptr(),
+    _call("apt_rmsnorm_mx4", index, stream, *args, eps, None if h is None else h.data_ptr(),
           None if y is None else y.data_ptr(), out.data.data_ptr())
     return (out, h, y) if out_y else (out, h)
 
