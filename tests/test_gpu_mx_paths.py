@@ -242,3 +242,28 @@ def test_values_of_more_rows_than_a_launch_takes(M, K):
         p = slice(at, at + 60)
         want = ((2.0 * codes[p].double() + 1) * scale[p].double()[:, None]).half()
         assert torch.equal(got[p], want), at
+
+
+@pytest.mark.parametrize("kind", ["fp16", "bf16"])
+@pytest.mark.parametrize("M,K", [(4, 300), (2100, 96), (3, 33001)])
+@pytest.mark.parametrize("eps", [0.0, 1e-5])
+def test_norm_at_the_types_ends(M, K, kind, eps):
+    """Whole rows of the largest values (in bf16 the row's factor is a subnormal fp32 number), of the
+    smallest and of subnormal ones, and all of them mixed."""
+    info = torch.finfo(TYPES[kind])
+    sign = np.where(np.random.default_rng(K).random(K) < 0.5, -1.0, 1.0)
+    x = np.zeros((M, K))
+    x[0] = sign * float(info.max)
+    x[1] = sign * float(info.smallest_normal)
+    x[2] = sign * {"fp16": 2.0 ** -24, "bf16": 2.0 ** -133}[kind]
+    if M > 3:
+        x[3:] = np.where(np.arange(K) % 3 == 0, x[0], np.where(np.arange(K) % 3 == 1, x[1], x[2]))
+    h, y = ref.norm(x, None, None, eps, kind)
+    codes, scale, _, got_y = apt.rmsnorm_codes(dev(x, kind), None, 8, eps, out_y=True)
+    same(got_y, y)
+    want_c, want_s = ref.codes(y, 8)
+    same(scale, want_s)
+    assert np.array_equal(codes.cpu().numpy(), want_c)
+    op, _, got_y = apt.rmsnorm_mx4(dev(x, kind), None, eps, out_y=True)
+    same(got_y, y)
+    same_operand(op, *ref.quantize(y))
