@@ -126,16 +126,18 @@ apt_status_t apt_mx4_gemm_act(int M, int N, int K, const void* x, int x_type, in
  *   h    = T(x + residual) (x itself without a residual)
  *   f    = fp32(1 / sqrt(sum_k h[k]^2 / K + eps)), the sum and its root in fp64
  *   y[k] = T(fp32(fp32(h[k] * f) * gain[k])) (fp32(h[k] * f) without a gain)
- * so that y, and with it every code, is the same whatever order the row is
- * summed in.  apt_rmsnorm_codes then quantizes the row to q-bit codes,
- * 1 <= q <= 8, by the rule of apt_quantize_pack_activations_fp16:
+ * The fp64 value is good to a few parts in 2^50, whatever order the row is summed
+ * in: y and its codes follow the definition unless it lies that close to a border
+ * between two fp32 roundings, where f may be the neighbour.  apt_rmsnorm_codes then
+ * quantizes the row to q-bit codes, 1 <= q <= 8, by the rule of
+ * apt_quantize_pack_activations_fp16:
  *   scale = fp16(fp32(max_k |y[k]| / (2^q - 1)))
  *   code  = floor(y[k] / (2 scale)), in [-2^(q-1), 2^(q-1) - 1], value
  *           (2 code + 1) scale; 0 where the scale is 0
  * as apt_gemm_act and apt_gemm_decode take them (APT_ACT_CODES with a_scale); a
  * row whose y holds a NaN or an infinity, or whose scale would be infinite, gets
  * a NaN scale and codes 0.  apt_rmsnorm_mx4 quantizes y as apt_mx4_quantize does.
- *   type       APT_TYPE_FP16 or APT_TYPE_BF16: x, residual, gain, h and y
+ *   type       APT_TYPE_FP16 or APT_TYPE_BF16, of x, residual, gain, h and y alike
  *   x, residual  device, M rows of K with their strides in elements (>= K);
  *              residual NULL for none (its stride is then ignored)
  *   gain       device [K] or NULL
@@ -148,7 +150,8 @@ apt_status_t apt_mx4_gemm_act(int M, int N, int K, const void* x, int x_type, in
  *   mx         device, apt_mx4_bytes(M, K) bytes, 16-byte aligned
  * Errors: APT_ERR_INVALID_ARG for sizes < 1, q outside [1, 8], a stride < K, a
  * type other than the two, a negative or non-finite eps, NULL x, codes, scale or
- * mx, a y that is x, residual or h, or misaligned pointers; APT_ERR_UNSUPPORTED for K > 2^30; APT_ERR_HIP. */
+ * mx, a y that is x, residual or h, or misaligned pointers; APT_ERR_UNSUPPORTED
+ * for K > 2^30; APT_ERR_HIP. */
 apt_status_t apt_rmsnorm_codes(int M, int K, int type, const void* x, int64_t x_stride,
                                const void* residual, int64_t residual_stride, const void* gain,
                                double eps, int q, void* h, void* y, int8_t* codes, uint16_t* scale,

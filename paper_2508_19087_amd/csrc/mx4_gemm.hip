@@ -95,7 +95,7 @@ double thin_time(int M, int N, int K, const Thin& t) {
 // 64 x 4096 x 11008 11.6, 9.3, 7.7, 10.1, 12.5; 256 x 1024 x 11008 10.0, 8.5, 7.4, 9.7, 12.3; 128 x
 // 4096 x 11008 19.1, 15.1, 11.4, 10.3, 12.5; 256 x 4096 x 11008 34, 26, 18.8, 15.8, 13.3).  Among
 // the tiles a large one costs fewer loads per MFMA and a small one fills the chip:
-// 2048 x 11008 x 4096 takes 46 us at 128 x 256 and 59, 56, 64, 90 at 256 x 256,
+// 2048 x 11008 x 4096 takes 46 us at 128 x 256 and 58, 56, 64, 90 at 256 x 256,
 // 128, 64 and 32 x 128; 333 x 5003 x 2999 7.3 us at 64 x 128, 9.1 and 11.9 at 128 x
 // 128 and 128 x 256; 1024 x 4096 x 11008 25 at 128 x 128 and 31 at 128 x 256.
 int kernel_of(int M, int N, int K) {

@@ -151,7 +151,8 @@ __global__ __launch_bounds__(kWave* kWaves) void dequantize_kernel(Rows a) {
 }
 
 // Row-major codes and scale bytes into the operand (or back), a thread per
-// block: once per model, so nothing of it is tuned.
+// block: once per model, so nothing of it is tuned (11008 x 4096, 24 MB in and out:
+// 49 us, and back 47, where a large copy takes 9).
 __global__ __launch_bounds__(256) void pack_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales,
                                                    int rows, int K, Operand o) {
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;

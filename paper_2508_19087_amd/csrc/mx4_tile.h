@@ -7,18 +7,21 @@
 //
 // A workgroup of four waves makes MB * 32 rows by NB * 128 columns; each wave
 // owns NB * 32 of the columns for all rows.  Its weights come straight from
-// memory into registers (no other wave needs them), a step ahead; the
-// activations, which all four waves need, go to LDS by direct loads, three steps
+// memory into registers (no other wave needs them), WD - 1 steps ahead (three for
+// 128 columns, one for 256, whose sums take the registers); the activations, which all four waves need, go to LDS by direct loads, three steps
 // ahead in a ring of four stages, and each fragment is read back two MFMA groups
 // before its use.  One barrier per step, in its middle: it makes the next step's
 // stage visible early enough that the first fragments and scales of that step
 // are read before this one ends, and it frees the stage of the step before.
 //
 // 2048 x 11008 x 4096 (128 x 256 tiles, bf16 output) takes 46 to 47 us in a graph,
-// 3.9 to 4.0 PFLOP/s, 16384 cubed 1755 us or 5.0.  Its MFMAs alone take 34 us: with
-// all units at dense products of random codes the clock falls to 1.5 to 1.6 GHz.
-// The rest is the last, partly filled round, and the loads' way into the unit (66
-// bytes a ns); which tiles share their weights in the cache makes no difference.
+// 3.9 to 4.0 PFLOP/s, 16384 cubed 1755 to 1790 us or 4.9 to 5.0.  Clock stamps in
+// the kernel: it runs at 1.50 to 1.55 GHz, with all units at dense products of
+// random codes (16384 cubed: 1.37 to 1.42).  Its MFMAs alone, in the same two rounds
+// of tiles, the second a third full, take 33 us at 1.6 to 1.7.  The rest is the
+// epilogues, 3.9 us in each round, and waits for loads: a tile takes 39600 cycles,
+// its MFMAs alone 27500.  Which tiles share their weights in the cache makes no
+// difference.
 // With about a tile per unit the ends count: the first step begins when its own
 // loads have landed, not those of the three that follow (256 x 11008 x 4096 10.6
 // us instead of 11.2, 333 x 5003 x 2999 7.3 instead of 7.6).
@@ -266,7 +269,8 @@ __global__ __launch_bounds__(kTileWaves* kWave, (MB * NB >= 12 ? 1 : 2)) void ti
 
   // ---- epilogue: through the wave's slot (stage `wave`), so that stores are whole
   // runs of all its columns of an output row (2048 x 11007 x 4096 into fp32, whose
-  // rows share lines: 75 us with runs of 256 bytes, 79 with two of 128).  The MFMA
+  // rows share lines: 75 to 77 us with runs of 256 bytes, 79 with two of 128; 2048 x
+  // 11008 x 4096, whose rows do not, 52).  The MFMA
   // leaves lane (r, h) columns 8 g + 4 h + 0..3 of row r.
   __builtin_amdgcn_s_waitcnt(0x0070);  // the last (unused) loads have landed
   __builtin_amdgcn_s_barrier();

@@ -7,8 +7,9 @@
 // between its passes (sum of squares, largest magnitude of y, codes), each
 // thread holding NV vectors of 8 elements; rows longer than the registers
 // reach (NV = 0) are read again in each pass.  In a graph 2048 x 4096 into codes
-// takes 13.2 us (59 MB, 4.5 TB/s; a large copy 5.2), into MX4 12.3, 1 x 4096 3.3
-// and 3.0: a launch and one trip to memory.
+// takes 13.0 us (59 MB, 4.5 TB/s; a large copy 5.1 to 5.2), into MX4 11.9, 1 x 4096
+// 3.2 and 3.0: a launch and one trip to memory.  Traced among other kernels 13.7 and
+// 12.3.
 //
 // The sum of squares runs in fp64.  A quantizer is a step function, and a y
 // that moved by one rounding with the order of its row's sum would now and then

@@ -395,7 +395,9 @@ def rmsnorm_codes(x, gain, q: int, eps: float, residual=None, h=None, out_y: boo
     """RMS norm of x + residual (fp16 or bf16 [M][K]) with `gain` [K] (or None), quantized per row to
     q-bit codes as gemm_act and gemm_decode take them.  Returns (codes int8 [M][K], fp16 scales [M],
     h), and y behind them with out_y: h is x + residual, written to `h` where one is given (x or the
-    residual themselves among them), to a new tensor where there is a residual, else None."""
+    residual itself, or a tensor that overlaps no input), to a new tensor where there is a residual,
+    else None.  The residual and the gain have x's type; rows in more dimensions are for the caller to
+    flatten."""
     torch = _torch()
     if not 1 <= q <= 8:
         _refuse("rmsnorm_codes", "codes of %s bits" % (q, ))
