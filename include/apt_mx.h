@@ -107,15 +107,16 @@ apt_status_t apt_mx4_select(int M, int N, int K, int* rows, int* columns);
 /* C = A * W^T with the activations given unpacked and quantized inside the call
  * as apt_mx4_quantize does; the result equals that of apt_mx4_quantize followed
  * by apt_mx4_gemm, bit for bit.  Up to 16 rows of together 16384 elements (rows
- * padded to 256) are quantized by the product's kernel itself, three rows or more
- * while these elements times N / 16 are at most 2^24; others go through the
- * workspace.
+ * padded to 256) can be quantized by the product's kernel itself, which needs no
+ * workspace; from three rows on, where these elements times N / 16 are more than
+ * 2^24, quantizing them into a workspace first is faster, and is done where there
+ * is one.  Other rows need it.
  *   x, x_type, x_stride  as apt_mx4_quantize, M rows
  *   workspace, workspace_bytes  device scratch of at least
  *               apt_mx4_gemm_act_workspace_bytes(M, N, K) bytes, 16-byte aligned
- *               (NULL when 0); overwritten; calls sharing it must not overlap in time
- * Errors as apt_mx4_quantize and apt_mx4_gemm, and APT_ERR_WORKSPACE when the
- * workspace is missing or too small. */
+ *               (ignored when 0); overwritten; calls sharing it must not overlap in time
+ * Errors as apt_mx4_quantize and apt_mx4_gemm, and APT_ERR_WORKSPACE when a
+ * workspace that is needed is missing or too small. */
 size_t apt_mx4_gemm_act_workspace_bytes(int M, int N, int K);
 apt_status_t apt_mx4_gemm_act(int M, int N, int K, const void* x, int x_type, int64_t x_stride,
                               const void* w_mx, int type, void* c, void* workspace,

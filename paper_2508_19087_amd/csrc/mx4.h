@@ -245,8 +245,10 @@ hipError_t launch_dequantize_codes(const int8_t* codes, const uint16_t* scale, i
 int64_t gemm_tiles(int M, int N, int K);
 void gemm_block(int M, int N, int K, int* rows, int* columns);
 hipError_t launch_gemm(int M, int N, int K, const Operand& a, const Operand& w, int type, void* c, hipStream_t s);
-// The same from rows, quantized in the product's kernel, where gemm_takes_rows.
-bool gemm_takes_rows(int M, int N, int K);
+// The same from rows, quantized in the product's kernel, where gemm_takes_rows;
+// gemm_prefers_rows: and where that costs less than quantizing them first.
+bool gemm_takes_rows(int M, int K);
+bool gemm_prefers_rows(int M, int N, int K);
 hipError_t launch_gemm_rows(int M, int N, int K, const void* x, int x_type, int64_t x_stride, const Operand& w, int type,
                             void* c, hipStream_t s);
 

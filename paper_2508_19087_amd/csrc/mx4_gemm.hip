@@ -33,7 +33,8 @@ constexpr double kTileEnds = 1.9;
 constexpr double kUnits = 256.0;  // compute units
 
 // Activations given as rows are quantized by the few-row kernel's workgroups
-// themselves, each on its own, up to kFusedElements elements (rows padded to steps).
+// themselves, each on its own, up to kFusedElements elements (rows padded to steps)
+// where that is the faster way.
 // The conversion takes 0.8 us per 4096 elements and saves a launch, which is 1.5 us
 // of a graph and 4 to 5 us of a call's time on the host.  Fused and not, in a graph
 // and by itself: 1 x 11008 x 4096 6.2 and 8.5, 7.3 and 12.5 us; 3 x 11008 x 4096 7.9 and 8.5, 7.6
@@ -182,9 +183,9 @@ hipError_t launch_gemm(int M, int N, int K, const Operand& a, const Operand& w, 
   }
 }
 
-bool gemm_takes_rows(int M, int N, int K) {
-  const int64_t elements = (int64_t)M * steps(K) * kStep;
-  return M <= 16 && elements <= kFusedElements && (M < kFusedRows || elements * groups(N) <= kFusedWork);
+bool gemm_takes_rows(int M, int K) { return M <= 16 && (int64_t)M * steps(K) * kStep <= kFusedElements; }
+bool gemm_prefers_rows(int M, int N, int K) {
+  return gemm_takes_rows(M, K) && (M < kFusedRows || (int64_t)M * steps(K) * kStep * groups(N) <= kFusedWork);
 }
 
 hipError_t launch_gemm_rows(int M, int N, int K, const void* x, int x_type, int64_t x_stride, const Operand& w, int type,

@@ -118,7 +118,7 @@ apt_status_t apt_mx4_select(int M, int N, int K, int* rows, int* columns) {
 }
 
 size_t apt_mx4_gemm_act_workspace_bytes(int M, int N, int K) {
-  if (!sizes_ok(M, N, K) || apt::mx4::gemm_takes_rows(M, N, K)) return 0;
+  if (!sizes_ok(M, N, K) || apt::mx4::gemm_prefers_rows(M, N, K)) return 0;
   return apt::mx4::operand_bytes(M, K);
 }
 
@@ -130,8 +130,10 @@ apt_status_t apt_mx4_gemm_act(int M, int N, int K, const void* x, int x_type, in
   hipStream_t s = static_cast<hipStream_t>(stream);
   const apt::mx4::Operand w = apt::mx4::operand(w_mx, N, K);
   const size_t need = apt_mx4_gemm_act_workspace_bytes(M, N, K);
-  if (need == 0) return hip_status(apt::mx4::launch_gemm_rows(M, N, K, x, x_type, x_stride, w, type, c, s));
-  if (workspace == nullptr || workspace_bytes < need) return APT_ERR_WORKSPACE;
+  const bool short_of_space = workspace == nullptr || workspace_bytes < need;
+  if (need == 0 || (apt::mx4::gemm_takes_rows(M, K) && (short_of_space || !aligned(workspace, 16))))
+    return hip_status(apt::mx4::launch_gemm_rows(M, N, K, x, x_type, x_stride, w, type, c, s));
+  if (short_of_space) return APT_ERR_WORKSPACE;
   if (!aligned(workspace, 16)) return APT_ERR_INVALID_ARG;
   const apt::mx4::Operand a = apt::mx4::operand(workspace, M, K);
   const hipError_t e = apt::mx4::launch_quantize(x, x_type, M, K, x_stride, a, s);

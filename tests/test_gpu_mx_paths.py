@@ -74,6 +74,22 @@ def test_few_rows_by_many_weight_rows(size):
     check_exact(apt.mx4_gemm_act(va.half(), w, torch.float32), want, size)
 
 
+@pytest.mark.parametrize("workspace", ["none", "short", "off alignment"])
+def test_few_rows_need_no_workspace(workspace):
+    """Rows that the product's kernel can quantize are taken without a workspace of use, where one would be faster."""
+    M, N, K = 4, 20011, 4000
+    need = apt.apt_mx4_gemm_act_workspace_bytes(M, N, K)
+    assert need == apt.apt_mx4_bytes(M, K)
+    x, w = dev(rows(1, M, K, "bf16", 1.0), "bf16"), packed(*random_mx4(2, N, K, 118, 121))
+    buf = torch.full((need + 64, ), 0xA5, dtype=torch.uint8, device="cuda")
+    ptr, n = {"none": (None, 0), "short": (buf.data_ptr(), need - 1), "off alignment": (buf.data_ptr() + 8, need)}[workspace]
+    c = torch.empty((M, N), dtype=torch.bfloat16, device="cuda")
+    apt.check(apt.apt_mx4_gemm_act(M, N, K, x.data_ptr(), apt.APT_TYPE_BF16, K, w.data.data_ptr(), apt.APT_TYPE_BF16,
+                                   c.data_ptr(), ptr, n, stream()), "apt_mx4_gemm_act")
+    check_exact(c, apt.mx4_gemm_act(x, w), workspace)
+    assert (buf == 0xA5).all()
+
+
 SOME = [(5, 20, 703), (17, 2052, 208), (17, 4206, 2120), (34, 5672, 4797), (33, 20, 353), (4100, 133, 686),
         (193, 8225, 436), (457, 8194, 473), (1089, 7413, 2770)]
 
