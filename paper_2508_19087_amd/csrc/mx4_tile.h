@@ -8,11 +8,12 @@
 // A workgroup of four waves makes MB * 32 rows by NB * 128 columns; each wave
 // owns NB * 32 of the columns for all rows.  Its weights come straight from
 // memory into registers (no other wave needs them), WD - 1 steps ahead (three for
-// 128 columns, one for 256, whose sums take the registers); the activations, which all four waves need, go to LDS by direct loads, three steps
-// ahead in a ring of four stages, and each fragment is read back two MFMA groups
-// before its use.  One barrier per step, in its middle: it makes the next step's
-// stage visible early enough that the first fragments and scales of that step
-// are read before this one ends, and it frees the stage of the step before.
+// 128 columns, one for 256, whose sums take the registers); the activations,
+// which all four waves need, go to LDS by direct loads, three steps ahead in a
+// ring of four stages, and each fragment is read back two MFMA groups before its
+// use.  One barrier per step, in its middle: it makes the next step's stage visible
+// early enough that the first fragments and scales of that step are read before
+// this one ends, and it frees the stage of the step before.
 //
 // 2048 x 11008 x 4096 (128 x 256 tiles, bf16 output) takes 46 to 47 us in a graph,
 // 3.9 to 4.0 PFLOP/s, 16384 cubed 1755 to 1790 us or 4.9 to 5.0.  Clock stamps in
